@@ -326,6 +326,137 @@ int ff8_swiglu_bwd_quant_fp8a(const ff8_e4m3* a_q, const float* a_s, const ff8_b
 int ff8_unpermute(const ff8_bf16* y_perm, const int32_t* row_map, const float* row_w, int64_t T, int k,
                   int64_t H, int64_t M_cap, ff8_bf16* y, void* stream);
 
+/* ---- the router, and rows sorted by expert without a cast ---- */
+
+/* Score functions of the router. */
+enum ff8_score {
+  FF8_SCORE_SOFTMAX = 0, /* softmax over the E logits */
+  FF8_SCORE_SIGMOID = 1  /* sigmoid of each logit */
+};
+
+/*
+ * ff8_router_topk -- the k experts of each token and their routing weights (the topk_idx and
+ *   probs of ff8_permute_quant, ff8_unpermute and ff8_route) from the router's logits.
+ *   logits   [T, E] float32.  -inf masks an expert; a NaN logit is never chosen (and makes the
+ *            token's softmax weights NaN).
+ *   bias     [E] float32 or NULL.  Experts are chosen by the largest score + bias (in float64; an expert whose
+ *            bias is -inf or NaN is never chosen), or, without a bias, by the largest logit; equal ones by the lower index.
+ *            The bias does not enter the weights.
+ *   topk_idx [T, k] int32, in descending order of choice; -1 where fewer than k experts can be chosen.
+ *   probs    [T, k] float32: scale * score, or with normalize = 1 scale * score / (sum of the chosen
+ *            scores); 0 where topk_idx is -1.  Normalized weights stay exact where the scores
+ *            themselves underflow.
+ * Requires 1 <= k <= E <= 1024, k <= 64, score an ff8_score, normalize 0 or 1, scale finite, T * k < 2^31.
+ */
+int ff8_router_topk(const float* logits, const float* bias, int64_t T, int E, int k, int score, int normalize,
+                    float scale, int32_t* topk_idx, float* probs, void* stream);
+/* The same from bf16 logits. */
+int ff8_router_topk_bf16(const ff8_bf16* logits, const float* bias, int64_t T, int E, int k, int score, int normalize,
+                         float scale, int32_t* topk_idx, float* probs, void* stream);
+
+/*
+ * ff8_router_topk_bwd -- the gradient of the logits through the routing weights (the choice itself has
+ *   none, nor has the bias): dlogits [T, E] from dprobs [T, k] float32, the logits and the forward's
+ *   topk_idx.  Every element of dlogits is written.  Slots of -1 add nothing, whatever dprobs holds
+ *   there.  score, normalize and scale as in the forward.  dlogits has the logits' type.
+ */
+int ff8_router_topk_bwd(const float* logits, const int32_t* topk_idx, const float* dprobs, int64_t T, int E, int k,
+                        int score, int normalize, float scale, float* dlogits, void* stream);
+int ff8_router_topk_bwd_bf16(const ff8_bf16* logits, const int32_t* topk_idx, const float* dprobs, int64_t T, int E,
+                             int k, int score, int normalize, float scale, ff8_bf16* dlogits, void* stream);
+
+/*
+ * ff8_route -- the routing maps of ff8_permute_quant_aligned alone (row_map, offsets, src_row, with
+ *   the same workspace and requirements): for calls that take the rows through src_row.
+ */
+int ff8_route(const int32_t* topk_idx, int64_t T, int k, int E, int32_t* row_map, int32_t* offsets, int32_t* src_row,
+              int64_t M_cap, void* workspace, size_t ws_bytes, int align, void* stream);
+
+/*
+ * ff8_permute_bf16 -- ff8_permute_quant_aligned without the cast: out[row_map[t, j]] = x[t], padding rows
+ *   zero, rows >= offsets[E] untouched.  Its gradient is ff8_unpermute without weights.
+ *   x [T, H] bf16; out [M_cap, H] bf16; x and out 16-byte aligned and apart from one another.  Maps,
+ *   reuse_map, workspace and requirements as there.
+ */
+int ff8_permute_bf16(const ff8_bf16* x, int64_t T, int64_t H, int k, int E, const int32_t* topk_idx, int reuse_map,
+                     int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap, ff8_bf16* out,
+                     void* workspace, size_t ws_bytes, int align, void* stream);
+
+/*
+ * ff8_permute_fp8 -- the same for rows that are FP8 already (tokens cast before their dispatch; paper
+ *   section 3.3.1 permutes and pads FP8 rows): xq [T, H] e4m3 with xs [T, H/128] go to q [M_cap, H], s
+ *   [M_cap, H/128] as they are; padding rows 0x00 with scale 2^-126.  Equal, byte for byte, to
+ *   ff8_permute_quant of the rows that ff8_quant_rowwise made xq from.
+ */
+int ff8_permute_fp8(const ff8_e4m3* xq, const float* xs, int64_t T, int64_t H, int k, int E, const int32_t* topk_idx,
+                    int reuse_map, int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap, ff8_e4m3* q,
+                    float* s, void* workspace, size_t ws_bytes, int align, void* stream);
+int ff8_permute_fp8_e8m0(const ff8_e4m3* xq, const ff8_e8m0* xs, int64_t T, int64_t H, int k, int E,
+                         const int32_t* topk_idx, int reuse_map, int32_t* row_map, int32_t* offsets, int32_t* src_row,
+                         int64_t M_cap, ff8_e4m3* q, ff8_e8m0* s, void* workspace, size_t ws_bytes, int align,
+                         void* stream);
+
+/*
+ * ff8_unpermute_bwd -- the gradient of ff8_unpermute with routing weights, in bf16 (ff8_permute_quant_dprobs
+ *   is its FP8 form):
+ *     dy_perm[row_map[t, j]] = bf16(row_w[t, j] * dy[t]),  padding rows zero,
+ *     dprobs[t, j] = sum_h dy[t, h] * y_perm[row_map[t, j], h] in float32, 0 for a dropped slot.
+ *   dy [T, H] bf16; row_w, dprobs [T, k] float32; row_map, offsets, src_row as the forward's; y_perm, dy_perm
+ *   [M_cap, H] bf16 (16-byte aligned; rows >= offsets[E] neither read nor written).  y_perm and dprobs may
+ *   both be NULL: dy_perm alone.  Requires k <= 64.
+ */
+int ff8_unpermute_bwd(const ff8_bf16* dy, const float* row_w, int64_t T, int64_t H, int k, int E,
+                      const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
+                      ff8_bf16* dy_perm, const ff8_bf16* y_perm, float* dprobs, void* stream);
+
+/* ---- 4-bit expert weights (serving) ---- */
+
+/*
+ * ff8_quant_mxfp4 -- MXFP4 quantization along the columns: e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6, bit 3 the
+ *   sign), two a byte with the lower column in the low nibble, and one UE8M0 scale for 32 columns.
+ *   w [rows, cols] bf16, finite; q [rows, cols/2]; s [rows, cols/32].
+ *   A group's T is the smallest integer >= -126 with max|w| <= 6 * 2^T (no value saturates; an all-zero group
+ *   gets -126), the rule of the e4m3 scales; codes are rounded to nearest, ties to even, sign kept.
+ *   rows >= 1, cols a multiple of 128, rows * cols < 2^35.
+ */
+int ff8_quant_mxfp4(const ff8_bf16* w, int64_t rows, int64_t cols, uint8_t* q, ff8_e8m0* s, void* stream);
+
+/*
+ * ff8_pack_mxfp4 -- MXFP4 weights in the order in which the products read them, once per set of weights.
+ *   q [rows, cols/2], s [rows, cols/32] as above (a stack of E expert weights [E, N, K] is rows = E*N).
+ *   tq [rows/16, cols/128, 64, 16]: bytes 16 l .. 16 l + 15 of a tile are row l % 16, columns 32 (l / 16) ..
+ *   + 31 of its 16 rows x 128 columns; ts [rows/16, cols/128, 64]: entry l is their scale.
+ *   rows and cols multiples of 128, rows * cols < 2^37; q and tq 16-byte aligned and apart from one another.
+ */
+int ff8_pack_mxfp4(const uint8_t* q, const ff8_e8m0* s, int64_t rows, int64_t cols, uint8_t* tq, ff8_e8m0* ts,
+                   void* stream);
+
+/*
+ * ff8_grouped_gemv_mxfp4 -- products of grouped rows with their expert's 4-bit weights, made for a few rows
+ *   per expert (a decoding step), where the weights are the traffic; right for any number.
+ *     out[m, n] = sum_k x[m, k] * D(w_e)[n, k] for m in expert e's rows,
+ *   bf16 activations, float32 sums, rounded once to bf16.
+ *   tq, ts   the weights [E, N, K] as ff8_pack_mxfp4 lays them out.  Every code * 2^T must be finite in bf16
+ *            (a scale byte of 255 is NaN).
+ *   src_row  [M_cap] or NULL (every row below offsets[E] holds data).  With it, rows whose entry is -1 are
+ *            padding: nothing of x is read for them, and out gets zeros.
+ *   top_k    0: x [x_rows = M_cap, K] holds the grouped rows.  k >= 1: x [x_rows = T, K] holds the tokens, and row m
+ *            takes token src_row[m] / top_k (src_row required): no permute is needed in front.
+ *   out      [M_cap, N] bf16; rows >= offsets[E] untouched.
+ *   E <= 1024; M_cap, N, K multiples of 128; x_rows and M_cap below 2^31; x, tq, ts and out 16-byte aligned.
+ */
+int ff8_grouped_gemv_mxfp4(const ff8_bf16* x, int64_t x_rows, const uint8_t* tq, const ff8_e8m0* ts,
+                           const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap, int64_t N,
+                           int64_t K, ff8_bf16* out, void* stream);
+
+/*
+ * ff8_grouped_gemv_mxfp4_swiglu -- the same with weights [E, 2I, K] ([gate | up]) and SwiGLU on the float32
+ *   sums: h[m, i] = silu(g) * u with g = row i and u = row I + i, rounded once to bf16.  h [M_cap, I].
+ */
+int ff8_grouped_gemv_mxfp4_swiglu(const ff8_bf16* x, int64_t x_rows, const uint8_t* tq, const ff8_e8m0* ts,
+                                  const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap,
+                                  int64_t I, int64_t K, ff8_bf16* h, void* stream);
+
 /* ---- UE8M0 scale storage ----
  * Paper section 2.1 names UE8M0 (unsigned, 8 exponent bits, no mantissa) as the scale format of
  * its recipe, and the power-of-two constraint of section 3.1 makes every scale exactly such a

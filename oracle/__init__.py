@@ -23,9 +23,11 @@ moe     fused permute+pad+quantize, grouped GEMMs (fprop/dgrad/wgrad), fused
         SwiGLU+quantize and its backward twin, unpermute (paper sections 3.2 and
         3.3).
 layer   the whole expert layer forward+backward, stage by stage (section 3.2).
+router  top-k choice and routing weights from logits, and their gradient.
+mxfp4   4-bit weights with group scales, their tile order and the products with them.
 
 Parity status: every function is pinned by ``tests/test_oracle_*.py``; no
 function is "parity unpinned".
 """
 
-from . import codec, quant, sat, moe, layer  # noqa: F401
+from . import codec, quant, sat, moe, layer, router, mxfp4  # noqa: F401

@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -39,6 +40,9 @@ hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
 #define REQUIRE_PTR(p) \
   if ((p) == nullptr) return fail(FF8_ERR_NULL, "%s: argument '%s' is NULL", __func__, #p)
+#define REQUIRE_ALIGNED(p)                              \
+  if (reinterpret_cast<uintptr_t>(p) % 16 != 0)         \
+  return fail(FF8_ERR_ARG, "%s: argument '%s' is not 16-byte aligned", __func__, #p)
 #define REQUIRE_SHAPE(cond) \
   if (!(cond)) return fail(FF8_ERR_SHAPE, "%s: shape check failed: %s", __func__, #cond)
 #define REQUIRE_ARG(cond) \
@@ -358,6 +362,191 @@ int ff8_unpermute(const ff8_bf16* y_perm, const int32_t* row_map, const float* r
     REQUIRE_PTR(y_perm); REQUIRE_PTR(row_map); REQUIRE_PTR(y);
   }
   return hip_status(ff8::launch_unpermute(y_perm, row_map, row_w, T, k, H, M_cap, y, as_stream(stream)), __func__);
+}
+
+/* ---- the router, and rows sorted by expert without a cast ---- */
+
+}  // extern "C"
+
+static int router_validate(const char* fn, const void* logits, int64_t T, int E, int k, int score, int normalize,
+                           float scale, const void* topk_idx, const void* weights, const void* out) {
+  if (!(k >= 1 && k <= E && E <= 1024 && k <= 64)) return fail(FF8_ERR_ARG, "%s: need 1 <= k <= E <= 1024, k <= 64", fn);
+  if (score != FF8_SCORE_SOFTMAX && score != FF8_SCORE_SIGMOID) return fail(FF8_ERR_ARG, "%s: unknown score", fn);
+  if (!(normalize == 0 || normalize == 1)) return fail(FF8_ERR_ARG, "%s: normalize must be 0 or 1", fn);
+  if (!std::isfinite(scale)) return fail(FF8_ERR_ARG, "%s: scale must be finite", fn);
+  if (!(T >= 0 && T < ((int64_t)1 << 31) && T * k < ((int64_t)1 << 31)))
+    return fail(FF8_ERR_SHAPE, "%s: need T >= 0 and T * k < 2^31", fn);
+  if (T > 0 && (!logits || !topk_idx || !weights || !out)) return fail(FF8_ERR_NULL, "%s: a tensor is NULL", fn);
+  return FF8_OK;
+}
+
+extern "C" {
+
+int ff8_router_topk(const float* logits, const float* bias, int64_t T, int E, int k, int score, int normalize,
+                    float scale, int32_t* topk_idx, float* probs, void* stream) {
+  const int rc = router_validate(__func__, logits, T, E, k, score, normalize, scale, topk_idx, probs, probs);
+  if (rc != FF8_OK) return rc;
+  return hip_status(ff8::launch_router_topk(logits, bias, T, E, k, score == FF8_SCORE_SIGMOID, normalize != 0, scale,
+                                            topk_idx, probs, as_stream(stream)),
+                    __func__);
+}
+
+int ff8_router_topk_bf16(const ff8_bf16* logits, const float* bias, int64_t T, int E, int k, int score, int normalize,
+                         float scale, int32_t* topk_idx, float* probs, void* stream) {
+  const int rc = router_validate(__func__, logits, T, E, k, score, normalize, scale, topk_idx, probs, probs);
+  if (rc != FF8_OK) return rc;
+  return hip_status(ff8::launch_router_topk(logits, bias, T, E, k, score == FF8_SCORE_SIGMOID, normalize != 0, scale,
+                                            topk_idx, probs, as_stream(stream)),
+                    __func__);
+}
+
+int ff8_router_topk_bwd(const float* logits, const int32_t* topk_idx, const float* dprobs, int64_t T, int E, int k,
+                        int score, int normalize, float scale, float* dlogits, void* stream) {
+  const int rc = router_validate(__func__, logits, T, E, k, score, normalize, scale, topk_idx, dprobs, dlogits);
+  if (rc != FF8_OK) return rc;
+  return hip_status(ff8::launch_router_topk_bwd(logits, topk_idx, dprobs, T, E, k, score == FF8_SCORE_SIGMOID,
+                                                normalize != 0, scale, dlogits, as_stream(stream)),
+                    __func__);
+}
+
+int ff8_router_topk_bwd_bf16(const ff8_bf16* logits, const int32_t* topk_idx, const float* dprobs, int64_t T, int E,
+                             int k, int score, int normalize, float scale, ff8_bf16* dlogits, void* stream) {
+  const int rc = router_validate(__func__, logits, T, E, k, score, normalize, scale, topk_idx, dprobs, dlogits);
+  if (rc != FF8_OK) return rc;
+  return hip_status(ff8::launch_router_topk_bwd(logits, topk_idx, dprobs, T, E, k, score == FF8_SCORE_SIGMOID,
+                                                normalize != 0, scale, dlogits, as_stream(stream)),
+                    __func__);
+}
+
+int ff8_route(const int32_t* topk_idx, int64_t T, int k, int E, int32_t* row_map, int32_t* offsets, int32_t* src_row,
+              int64_t M_cap, void* workspace, size_t ws_bytes, int align, void* stream) {
+  const int rc = permute_validate(__func__, row_map, T, 128, k, E, topk_idx, 0, row_map, offsets, src_row, M_cap,
+                                  offsets, offsets, workspace, ws_bytes, align, true);
+  if (rc != FF8_OK) return rc;
+  return hip_status(ff8::launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace,
+                                      as_stream(stream)),
+                    __func__);
+}
+
+int ff8_permute_bf16(const ff8_bf16* x, int64_t T, int64_t H, int k, int E, const int32_t* topk_idx, int reuse_map,
+                     int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap, ff8_bf16* out,
+                     void* workspace, size_t ws_bytes, int align, void* stream) {
+  int rc = permute_validate(__func__, x, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, out, out,
+                            workspace, ws_bytes, align, true);
+  if (rc != FF8_OK) return rc;
+  REQUIRE_ALIGNED(x); REQUIRE_ALIGNED(out);
+  if (!reuse_map) {
+    rc = hip_status(ff8::launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace,
+                                      as_stream(stream)),
+                    __func__);
+    if (rc != FF8_OK) return rc;
+  }
+  return hip_status(ff8::launch_permute_bf16(x, T, H, k, E, row_map, offsets, src_row, M_cap, out, as_stream(stream)),
+                    __func__);
+}
+
+}  // extern "C"
+
+template <typename SC>
+static int permute_fp8(const char* fn, const ff8_e4m3* xq, const SC* xs, int64_t T, int64_t H, int k, int E,
+                       const int32_t* topk_idx, int reuse_map, int32_t* row_map, int32_t* offsets, int32_t* src_row,
+                       int64_t M_cap, ff8_e4m3* q, SC* s, void* workspace, size_t ws_bytes, int align, hipStream_t st) {
+  int rc = permute_validate(fn, xq, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, q, s, workspace,
+                            ws_bytes, align, true);
+  if (rc != FF8_OK) return rc;
+  if (T > 0 && !xs) return fail(FF8_ERR_NULL, "%s: xs is NULL", fn);
+  if ((reinterpret_cast<uintptr_t>(xq) | reinterpret_cast<uintptr_t>(q)) % 16 != 0)
+    return fail(FF8_ERR_ARG, "%s: xq and q must be 16-byte aligned", fn);
+  if (!reuse_map) {
+    rc = hip_status(ff8::launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace, st), fn);
+    if (rc != FF8_OK) return rc;
+  }
+  return hip_status(ff8::launch_permute_fp8(xq, xs, T, H, k, E, row_map, offsets, src_row, M_cap, q, s, st), fn);
+}
+
+// Common to the two 4-bit products; N counts weight rows.
+static int gemv_mxfp4(const char* fn, const ff8_bf16* x, int64_t x_rows, const uint8_t* tq, const ff8_e8m0* ts,
+                      const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap, int64_t N,
+                      int64_t K, bool swiglu, ff8_bf16* out, void* stream) {
+  if (!(E >= 1 && E <= 1024)) return fail(FF8_ERR_ARG, "%s: need 1 <= E <= 1024", fn);
+  if (top_k < 0) return fail(FF8_ERR_ARG, "%s: top_k must not be negative", fn);
+  if (!(mult128(M_cap) && mult128(N) && mult128(K)) || (swiglu && !mult128(N / 2)))
+    return fail(FF8_ERR_SHAPE, "%s: M_cap, the weights' rows and K must be multiples of 128", fn);
+  if (!(M_cap < ((int64_t)1 << 31) && x_rows >= 0 && x_rows < ((int64_t)1 << 31)))
+    return fail(FF8_ERR_SHAPE, "%s: M_cap and x_rows must be below 2^31", fn);
+  if (top_k == 0 && x_rows != M_cap) return fail(FF8_ERR_SHAPE, "%s: grouped rows: x_rows must be M_cap", fn);
+  if ((x_rows > 0 && !x) || !tq || !ts || !offsets || !out) return fail(FF8_ERR_NULL, "%s: a tensor is NULL", fn);
+  if (top_k > 0 && !src_row) return fail(FF8_ERR_NULL, "%s: src_row is NULL", fn);
+  if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(tq) | reinterpret_cast<uintptr_t>(ts) |
+       reinterpret_cast<uintptr_t>(out)) % 16 != 0)
+    return fail(FF8_ERR_ARG, "%s: x, tq, ts and out must be 16-byte aligned", fn);
+  return hip_status(ff8::launch_grouped_gemv_mxfp4(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, swiglu,
+                                                   out, as_stream(stream)),
+                    fn);
+}
+
+extern "C" {
+
+int ff8_permute_fp8(const ff8_e4m3* xq, const float* xs, int64_t T, int64_t H, int k, int E, const int32_t* topk_idx,
+                    int reuse_map, int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap, ff8_e4m3* q,
+                    float* s, void* workspace, size_t ws_bytes, int align, void* stream) {
+  return permute_fp8(__func__, xq, xs, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, q, s,
+                     workspace, ws_bytes, align, as_stream(stream));
+}
+
+int ff8_permute_fp8_e8m0(const ff8_e4m3* xq, const ff8_e8m0* xs, int64_t T, int64_t H, int k, int E,
+                         const int32_t* topk_idx, int reuse_map, int32_t* row_map, int32_t* offsets, int32_t* src_row,
+                         int64_t M_cap, ff8_e4m3* q, ff8_e8m0* s, void* workspace, size_t ws_bytes, int align,
+                         void* stream) {
+  return permute_fp8(__func__, xq, xs, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, q, s,
+                     workspace, ws_bytes, align, as_stream(stream));
+}
+
+int ff8_unpermute_bwd(const ff8_bf16* dy, const float* row_w, int64_t T, int64_t H, int k, int E,
+                      const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
+                      ff8_bf16* dy_perm, const ff8_bf16* y_perm, float* dprobs, void* stream) {
+  const int rc = permute_validate(__func__, dy, T, H, k, E, nullptr, 1, row_map, offsets, src_row, M_cap, dy_perm,
+                                  dy_perm, nullptr, 0, 16, true);
+  if (rc != FF8_OK) return rc;
+  REQUIRE_ARG(k <= 64);
+  if (T > 0) {
+    REQUIRE_PTR(row_w);
+    if ((y_perm == nullptr) != (dprobs == nullptr))
+      return fail(FF8_ERR_NULL, "%s: y_perm and dprobs go together", __func__);
+  }
+  REQUIRE_ALIGNED(dy); REQUIRE_ALIGNED(dy_perm); REQUIRE_ALIGNED(y_perm);
+  return hip_status(ff8::launch_unpermute_bwd(dy, row_w, T, H, k, E, row_map, offsets, src_row, M_cap, dy_perm, y_perm,
+                                              dprobs, as_stream(stream)),
+                    __func__);
+}
+
+/* ---- 4-bit expert weights ---- */
+
+int ff8_quant_mxfp4(const ff8_bf16* w, int64_t rows, int64_t cols, uint8_t* q, ff8_e8m0* s, void* stream) {
+  REQUIRE_PTR(w); REQUIRE_PTR(q); REQUIRE_PTR(s);
+  REQUIRE_SHAPE(rows >= 1 && mult128(cols) && rows < ((int64_t)1 << 35) / cols);
+  REQUIRE_ALIGNED(w); REQUIRE_ALIGNED(q);
+  return hip_status(ff8::launch_quant_mxfp4(w, rows, cols, q, s, as_stream(stream)), __func__);
+}
+
+int ff8_pack_mxfp4(const uint8_t* q, const ff8_e8m0* s, int64_t rows, int64_t cols, uint8_t* tq, ff8_e8m0* ts,
+                   void* stream) {
+  REQUIRE_PTR(q); REQUIRE_PTR(s); REQUIRE_PTR(tq); REQUIRE_PTR(ts);
+  REQUIRE_SHAPE(mult128(rows) && mult128(cols) && rows < ((int64_t)1 << 37) / cols);
+  REQUIRE_ALIGNED(q); REQUIRE_ALIGNED(tq); REQUIRE_ALIGNED(ts);
+  return hip_status(ff8::launch_pack_mxfp4(q, s, rows, cols, tq, ts, as_stream(stream)), __func__);
+}
+
+int ff8_grouped_gemv_mxfp4(const ff8_bf16* x, int64_t x_rows, const uint8_t* tq, const ff8_e8m0* ts,
+                           const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap, int64_t N,
+                           int64_t K, ff8_bf16* out, void* stream) {
+  return gemv_mxfp4(__func__, x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, false, out, stream);
+}
+
+int ff8_grouped_gemv_mxfp4_swiglu(const ff8_bf16* x, int64_t x_rows, const uint8_t* tq, const ff8_e8m0* ts,
+                                  const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap,
+                                  int64_t I, int64_t K, ff8_bf16* h, void* stream) {
+  return gemv_mxfp4(__func__, x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, 2 * I, K, true, h, stream);
 }
 
 /* ---- UE8M0 scale storage: the same operations with one scale byte T + 127 ---- */

@@ -66,6 +66,39 @@ int64_t max_h_dprobs();
 hipError_t launch_unpermute(const uint16_t* y_perm, const int32_t* row_map, const float* row_w, int64_t T, int k,
                             int64_t H, int64_t M_cap, uint16_t* y, hipStream_t st);
 
+// Router: sig / norm choose the score function and the normalization over the chosen.
+hipError_t launch_router_topk(const float* logits, const float* bias, int64_t T, int E, int k, bool sig, bool norm,
+                              float scale, int32_t* idx, float* probs, hipStream_t st);
+hipError_t launch_router_topk(const uint16_t* logits, const float* bias, int64_t T, int E, int k, bool sig, bool norm,
+                              float scale, int32_t* idx, float* probs, hipStream_t st);
+hipError_t launch_router_topk_bwd(const float* logits, const int32_t* idx, const float* dprobs, int64_t T, int E, int k,
+                                  bool sig, bool norm, float scale, float* dlogits, hipStream_t st);
+hipError_t launch_router_topk_bwd(const uint16_t* logits, const int32_t* idx, const float* dprobs, int64_t T, int E,
+                                  int k, bool sig, bool norm, float scale, uint16_t* dlogits, hipStream_t st);
+
+// Rows moved without a cast, by maps that are already built, and the gradient of the weighted return
+// (y_perm and dprobs both NULL: dy_perm alone).
+hipError_t launch_permute_bf16(const uint16_t* x, int64_t T, int64_t H, int k, int E, const int32_t* row_map,
+                               const int32_t* offsets, const int32_t* src_row, int64_t M_cap, uint16_t* out,
+                               hipStream_t st);
+hipError_t launch_permute_fp8(const uint8_t* xq, const float* xs, int64_t T, int64_t H, int k, int E,
+                              const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
+                              uint8_t* q, float* s, hipStream_t st);
+hipError_t launch_permute_fp8(const uint8_t* xq, const e8m0_t* xs, int64_t T, int64_t H, int k, int E,
+                              const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
+                              uint8_t* q, e8m0_t* s, hipStream_t st);
+hipError_t launch_unpermute_bwd(const uint16_t* dy, const float* row_w, int64_t T, int64_t H, int k, int E,
+                                const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
+                                uint16_t* dy_perm, const uint16_t* y_perm, float* dprobs, hipStream_t st);
+
+// MXFP4 weights: quantization, tile order, and the products (N: weight rows; with swiglu out has N / 2 columns).
+hipError_t launch_quant_mxfp4(const uint16_t* w, int64_t rows, int64_t cols, uint8_t* q, e8m0_t* s, hipStream_t st);
+hipError_t launch_pack_mxfp4(const uint8_t* q, const e8m0_t* s, int64_t rows, int64_t cols, uint8_t* tq, e8m0_t* ts,
+                             hipStream_t st);
+hipError_t launch_grouped_gemv_mxfp4(const uint16_t* x, int64_t x_rows, const uint8_t* tq, const e8m0_t* ts,
+                                     const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap,
+                                     int64_t N, int64_t K, bool swiglu, uint16_t* out, hipStream_t st);
+
 hipError_t launch_swiglu_quant(const uint16_t* a, const int32_t* offsets, int E, int64_t M_cap, int64_t I,
                                uint8_t* hq, float* hs, hipStream_t st);
 hipError_t launch_swiglu_quant(const uint16_t* a, const int32_t* offsets, int E, int64_t M_cap, int64_t I,

@@ -236,3 +236,69 @@ class ExpertLayerFP8:
         self.quantize_weights(w1, w2)
         self.forward(x, topk_idx, probs)
         return self.backward(dy, probs)
+
+
+class ExpertLayerFP4:
+    """Serving form of the expert layer: the forward alone, from the router's logits, with MXFP4 weights and
+    bf16 activations, for batches of up to `T` tokens.
+
+    A step is five calls: ff8_router_topk, ff8_route (groups padded to 16 rows), the up projection with SwiGLU
+    (which takes the tokens through the routing maps, so nothing is permuted), the down projection and the
+    weighted return.  Nothing is allocated after construction, and nothing synchronizes with the host."""
+
+    ALIGN = 16
+
+    def __init__(self, T, H, E, k, I, device="cuda", score="softmax", normalize=False, scale=1.0):
+        if score not in ff8.SCORES:
+            raise ValueError(f"score must be one of {sorted(ff8.SCORES)}")
+        if T < 1 or not 1 <= k <= min(E, 64) or E > 1024 or H % 128 or I % 128 or H < 128 or I < 128:
+            raise ValueError("need T >= 1, 1 <= k <= E <= 1024, k <= 64, H and I positive multiples of 128")
+        self.T, self.H, self.E, self.k, self.I = T, H, E, k, I
+        self.score, self.normalize, self.scale = score, normalize, scale
+        self.device = dev = torch.device(device)
+        M = self.rows(T)
+        tiles = lambda n, k_: (((E, n // 16, k_ // 128, 64, 16), _u8), ((E, n // 16, k_ // 128, 64), _u8))  # noqa: E731
+        spec = {"ws": ((max(1, ff8.ff8_permute_workspace_bytes(T, k, E)),), _u8),
+                "topk_idx": ((T, k), _i32), "probs": ((T, k), _f32), "row_map": ((T, k), _i32),
+                "offsets": ((E + 1,), _i32), "src_row": ((M,), _i32),
+                "h": ((M, I), _bf16), "y_perm": ((M, H), _bf16), "y": ((T, H), _bf16)}
+        spec["w1q"], spec["w1s"] = tiles(2 * I, H)
+        spec["w2q"], spec["w2s"] = tiles(H, I)
+        self.buf = _alloc(spec, dev)
+
+    def rows(self, T):
+        """Rows of the grouped buffers for a batch of T tokens."""
+        return ff8.ff8_rows_bound_aligned(T, self.k, self.E, self.ALIGN)
+
+    def nbytes(self):
+        return _nbytes(self.buf)
+
+    def quantize_weights(self, w1, w2):
+        """MXFP4 weights from bf16 w1 [E, 2I, H] ([gate | up]) and w2 [E, H, I]."""
+        for name, w, shape in (("w1", w1, (self.E, 2 * self.I, self.H)), ("w2", w2, (self.E, self.H, self.I))):
+            if tuple(w.shape) != shape:
+                raise ValueError(f"{name} must have shape {shape}, got {tuple(w.shape)}")
+            q = torch.empty((*shape[:2], shape[2] // 2), dtype=_u8, device=self.device)
+            s = torch.empty((*shape[:2], shape[2] // 32), dtype=_u8, device=self.device)
+            ff8.ff8_quant_mxfp4(w, q, s)
+            ff8.ff8_pack_mxfp4(q, s, self.buf[name + "q"], self.buf[name + "s"])
+
+    def load_weights(self, w1q, w1s, w2q, w2s):
+        """MXFP4 weights as checkpoints hold them: row-major codes [E, N, K / 2] and scales [E, N, K / 32]."""
+        ff8.ff8_pack_mxfp4(w1q, w1s, self.buf["w1q"], self.buf["w1s"])
+        ff8.ff8_pack_mxfp4(w2q, w2s, self.buf["w2q"], self.buf["w2s"])
+
+    def forward(self, x, logits, bias=None):
+        """y [T, H] (the layer's own buffer) of tokens x [T, H] with router logits [T, E]."""
+        T = x.shape[0]
+        if T > self.T:
+            raise ValueError(f"a batch of {T} tokens, the layer was made for {self.T}")
+        b, M = self.buf, self.rows(T)
+        idx, probs, row_map, y = b["topk_idx"][:T], b["probs"][:T], b["row_map"][:T], b["y"][:T]
+        src, h, y_perm = b["src_row"][:M], b["h"][:M], b["y_perm"][:M]
+        ff8.ff8_router_topk(logits, idx, probs, bias=bias, score=self.score, normalize=self.normalize, scale=self.scale)
+        ff8.ff8_route(idx, self.E, row_map, b["offsets"], src, b["ws"], align=self.ALIGN)
+        ff8.ff8_grouped_gemv_mxfp4_swiglu(x, b["w1q"], b["w1s"], b["offsets"], h, src_row=src, top_k=self.k)
+        ff8.ff8_grouped_gemv_mxfp4(h, b["w2q"], b["w2s"], b["offsets"], y_perm, src_row=src)
+        ff8.ff8_unpermute(y_perm, row_map, probs, y)
+        return y
