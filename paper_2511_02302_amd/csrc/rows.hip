@@ -6,9 +6,15 @@
 //   gradient  of the return y[t] = sum_j w[t, j] y_perm[row_map[t, j]]:
 //             dy_perm[row_map[t, j]] = bf16(w[t, j] dy[t]),  dw[t, j] = <dy[t], y_perm[row_map[t, j]]>.
 //
-// Both are bound by HBM: a token's row is read once, by one workgroup, and written to each of its k
-// rows (whole 16-byte pieces, consecutive lanes).  The first E workgroups of a launch fill the expert
-// groups' padding rows.  The routing maps are those of ff8_permute_quant.
+// Both are bound by HBM: one wave moves one row (16-byte pieces, consecutive lanes), eight waves a workgroup, so
+// that the k rows of a token are mostly written by one workgroup and its input row comes from HBM once and from
+// the XCD's L2 the other times.  A lane has up to eight pieces in flight before its first store.  At 16384
+// tokens x 7168 in bf16, k = 8 (2.1 GB) the sort takes 390 us, 5.4 TB/s: a workgroup per token that holds its row
+// in registers took 422, loads that alternate with stores 410, a row per workgroup 516, a wave per output row in
+// output order 548.  The gradient (4.0 GB) takes 758 us, 5.3 TB/s (772 with a workgroup per token).  Copying the
+// same rows in order reaches 5.8 TB/s and in the sorted order 5.5, so what is left is the order that the routing
+// gives.  The first E workgroups of a launch fill the expert groups' padding rows.
+// The routing maps are those of ff8_permute_quant.
 
 #include "ff8_device.hpp"
 #include "ff8_launch.hpp"
@@ -17,110 +23,131 @@ namespace ff8 {
 
 namespace {
 
-constexpr int kRowThreadsMax = 512;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kPieces = 8;  // 16-byte pieces that a lane has in flight
 
-// Zeros in the padding rows (src_row < 0) of expert e's group: fewer than 128, all among the group's
-// last 128.  row16: 16-byte pieces of a row; n_s: its scales (0 for bf16 rows).
+// Zeros in the padding rows (src_row < 0) of expert e's group: fewer than 128, all among the group's last 128.
+// Their numbers are collected in LDS first (two loads a lane instead of one before every row), then each wave
+// takes every eighth.  row16: 16-byte pieces of a row; n_s: its scales (0 for bf16 rows).
 template <typename S>
 __device__ __forceinline__ void pad_rows(int e, const int32_t* __restrict__ offsets, const int32_t* __restrict__ src_row,
-                                         int64_t row16, int n_s, u32x4* __restrict__ out, S* __restrict__ s_out) {
-  const int64_t g1 = offsets[e + 1], g0 = offsets[e];
-  const u32x4 z = {0u, 0u, 0u, 0u};
-  for (int64_t r = g1 - g0 > kTile ? g1 - kTile : g0; r < g1; ++r) {
-    if (src_row[r] >= 0) continue;
-    for (int64_t c = threadIdx.x; c < row16; c += blockDim.x) stnt16(out + r * row16 + c, z);
-    for (int c = threadIdx.x; c < n_s; c += blockDim.x) put_scale(&s_out[r * n_s + c], kTMin);
+                                         int64_t M_cap, int64_t row16, int n_s, u32x4* __restrict__ out,
+                                         S* __restrict__ s_out) {
+  __shared__ int rows[kTile];
+  __shared__ int n_rows;
+  const int64_t g0 = offsets[e], g1 = offsets[e + 1] < M_cap ? offsets[e + 1] : M_cap;
+  const int64_t r0 = g1 - g0 > kTile ? g1 - kTile : g0;
+  const int lane = threadIdx.x & 63;
+  if (threadIdx.x < 64) {
+    int n = 0;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int64_t r = r0 + 64 * half + lane;
+      const bool pad = r < g1 && src_row[r] < 0;
+      const unsigned long long m = __ballot(pad);
+      if (pad) rows[n + __popcll(m & ((1ull << lane) - 1))] = 64 * half + lane;
+      n += __popcll(m);
+    }
+    if (lane == 0) n_rows = n;
   }
+  __syncthreads();
+  const u32x4 z = {0u, 0u, 0u, 0u};
+  for (int i = threadIdx.x >> 6; i < n_rows; i += kWaves) {
+    const int64_t r = r0 + rows[i];
+    for (int64_t c = lane; c < row16; c += 64) stnt16(out + r * row16 + c, z);
+    for (int c = lane; c < n_s; c += 64) put_scale(&s_out[r * n_s + c], kTMin);
+  }
+}
+
+// The (token, slot) pair of a wave behind the E padding workgroups; the same for all its lanes.
+__device__ __forceinline__ int pair_of_wave(int E) {
+  return __builtin_amdgcn_readfirstlane((int)(blockIdx.x - E) * kWaves + (int)(threadIdx.x >> 6));
 }
 
 template <typename S>
-__global__ __launch_bounds__(kRowThreadsMax) void sort_rows_kernel(const u32x4* __restrict__ x,
-                                                                   const S* __restrict__ s, int64_t row16, int n_s,
-                                                                   int k, int E, const int32_t* __restrict__ row_map,
-                                                                   const int32_t* __restrict__ offsets,
-                                                                   const int32_t* __restrict__ src_row, int64_t M_cap,
-                                                                   u32x4* __restrict__ out, S* __restrict__ s_out) {
-  const int64_t t = (int64_t)blockIdx.x - E;
-  if (t < 0) {
-    pad_rows<S>((int)blockIdx.x, offsets, src_row, row16, n_s, out, s_out);
+__global__ __launch_bounds__(kThreads) void sort_rows_kernel(const u32x4* __restrict__ x, const S* __restrict__ s,
+                                                             int64_t row16, int n_s, int n_pairs, int k, int E,
+                                                             const int32_t* __restrict__ row_map,
+                                                             const int32_t* __restrict__ offsets,
+                                                             const int32_t* __restrict__ src_row, int64_t M_cap,
+                                                             u32x4* __restrict__ out, S* __restrict__ s_out) {
+  if ((int)blockIdx.x < E) {
+    pad_rows<S>((int)blockIdx.x, offsets, src_row, M_cap, row16, n_s, out, s_out);
     return;
   }
-  for (int64_t c = threadIdx.x; c < row16; c += blockDim.x) {
-    const u32x4 v = ldnt16(x + t * row16 + c);
-    for (int j = 0; j < k; ++j) {
-      const int row = row_map[t * k + j];
-      if (row >= 0 && row < M_cap) stnt16(out + row * row16 + c, v);
-    }
+  const int p = pair_of_wave(E), lane = threadIdx.x & 63;
+  if (p >= n_pairs) return;
+  const int64_t t = p / k, r = row_map[p];
+  if (r < 0 || r >= M_cap) return;
+  for (int64_t c0 = lane; c0 < row16; c0 += 64 * kPieces) {
+    u32x4 v[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (c0 + 64 * i < row16) v[i] = ld16(x + t * row16 + c0 + 64 * i);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (c0 + 64 * i < row16) stnt16(out + r * row16 + c0 + 64 * i, v[i]);
   }
-  for (int i = threadIdx.x; i < n_s * k; i += blockDim.x) {
-    const int j = i / n_s, c = i - j * n_s, row = row_map[t * k + j];
-    if (row >= 0 && row < M_cap) s_out[(int64_t)row * n_s + c] = s[t * n_s + c];
-  }
+  for (int c = lane; c < n_s; c += 64) s_out[r * n_s + c] = s[t * n_s + c];
 }
 
-// Sum of a dot product, fixed order: a lane's products in column order, a butterfly over the wave,
-// then the waves in order.
-constexpr int kMaxK = 64;
+// Sum of a dot product, fixed order: a lane's products in column order, then a butterfly over the wave.
 template <bool kDprobs>
-__global__ __launch_bounds__(kRowThreadsMax) void return_bwd_kernel(
-    const uint16_t* __restrict__ dy, const float* __restrict__ row_w, int64_t H, int k, int E,
+__global__ __launch_bounds__(kThreads) void return_bwd_kernel(
+    const u32x4* __restrict__ dy, const float* __restrict__ row_w, int64_t row16, int n_pairs, int k, int E,
     const int32_t* __restrict__ row_map, const int32_t* __restrict__ offsets, const int32_t* __restrict__ src_row,
-    int64_t M_cap, uint16_t* __restrict__ dy_perm, const uint16_t* __restrict__ y_perm, float* __restrict__ dprobs) {
-  __shared__ float part[kMaxK * (kRowThreadsMax / 64)];
-  const int64_t t = (int64_t)blockIdx.x - E, row8 = H / 8;
-  if (t < 0) {
-    pad_rows<e8m0_t>((int)blockIdx.x, offsets, src_row, row8, 0, reinterpret_cast<u32x4*>(dy_perm), nullptr);
+    int64_t M_cap, u32x4* __restrict__ dy_perm, const u32x4* __restrict__ y_perm, float* __restrict__ dprobs) {
+  if ((int)blockIdx.x < E) {
+    pad_rows<e8m0_t>((int)blockIdx.x, offsets, src_row, M_cap, row16, 0, dy_perm, nullptr);
     return;
   }
-  const int wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-  for (int j = 0; j < k; ++j) {
-    const int row = row_map[t * k + j];
-    const bool ok = row >= 0 && row < M_cap;  // uniform
-    float acc = 0.0f;
-    if (ok) {
-      const float w = row_w[t * k + j];
-      for (int64_t c = threadIdx.x; c < row8; c += blockDim.x) {
-        float v[8], y[8];
-        unpack_bf16x8(ld16(dy + t * H + c * 8), v);
-        u32x4 o;
+  const int p = pair_of_wave(E), lane = threadIdx.x & 63;
+  if (p >= n_pairs) return;
+  const int64_t t = p / k, r = row_map[p];
+  float acc = 0.0f;
+  if (r >= 0 && r < M_cap) {
+    const float w = row_w[p];
+    for (int64_t c0 = lane; c0 < row16; c0 += 64 * kPieces) {
+      u32x4 y[kPieces], d[kPieces];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(w * v[2 * i], w * v[2 * i + 1]);
-        stnt16(dy_perm + row * H + c * 8, o);
-        if (kDprobs) {
-          unpack_bf16x8(ldnt16(y_perm + row * H + c * 8), y);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc = fmaf(v[i], y[i], acc);
+      for (int u = 0; u < kPieces; ++u)
+        if (c0 + 64 * u < row16) {
+          if (kDprobs) y[u] = ldnt16(y_perm + r * row16 + c0 + 64 * u);
+          d[u] = ld16(dy + t * row16 + c0 + 64 * u);
         }
-      }
-    }
-    if (kDprobs) {
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) acc += __shfl_xor(acc, d);
-      if ((threadIdx.x & 63) == 0) part[j * (kRowThreadsMax / 64) + wave] = acc;
+      for (int u = 0; u < kPieces; ++u)
+        if (c0 + 64 * u < row16) {
+          u32x4 o;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float lo = bf16_lo(d[u][i]), hi = bf16_hi(d[u][i]);
+            o[i] = pack_bf16x2(w * lo, w * hi);
+            if (kDprobs) {
+              acc = fmaf(lo, bf16_lo(y[u][i]), acc);
+              acc = fmaf(hi, bf16_hi(y[u][i]), acc);
+            }
+          }
+          stnt16(dy_perm + r * row16 + c0 + 64 * u, o);
+        }
     }
   }
-  if (!kDprobs) return;
-  __syncthreads();
-  for (int j = threadIdx.x; j < k; j += blockDim.x) {
-    float sum = 0.0f;
-    for (int w = 0; w < n_waves; ++w) sum += part[j * (kRowThreadsMax / 64) + w];
-    dprobs[t * k + j] = sum;
+  if (kDprobs) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) acc += __shfl_xor(acc, d);
+    if (lane == 0) dprobs[p] = acc;
   }
 }
 
-// Threads of a one-token workgroup: one lane per 16-byte piece, whole waves, at most 512.
-unsigned row_threads(int64_t pieces) {
-  const int64_t n = (pieces + 63) / 64 * 64;
-  return (unsigned)(n < kRowThreadsMax ? n : kRowThreadsMax);
-}
+unsigned grid_of(int64_t n_pairs, int E) { return (unsigned)(E + (n_pairs + kWaves - 1) / kWaves); }
 
 template <typename S>
 hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_s, int k, int E, const int32_t* row_map,
                      const int32_t* offsets, const int32_t* src_row, int64_t M_cap, void* out, S* s_out,
                      hipStream_t st) {
-  sort_rows_kernel<S><<<(unsigned)(T + E), row_threads(row16), 0, st>>>(
-      static_cast<const u32x4*>(x), s, row16, n_s, k, E, row_map, offsets, src_row, M_cap, static_cast<u32x4*>(out),
-      s_out);
+  sort_rows_kernel<S><<<grid_of(T * k, E), kThreads, 0, st>>>(static_cast<const u32x4*>(x), s, row16, n_s, (int)(T * k),
+                                                              k, E, row_map, offsets, src_row, M_cap,
+                                                              static_cast<u32x4*>(out), s_out);
   return hipGetLastError();
 }
 
@@ -145,13 +172,15 @@ hipError_t launch_permute_fp8(const uint8_t* xq, const e8m0_t* xs, int64_t T, in
 hipError_t launch_unpermute_bwd(const uint16_t* dy, const float* row_w, int64_t T, int64_t H, int k, int E,
                                 const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
                                 uint16_t* dy_perm, const uint16_t* y_perm, float* dprobs, hipStream_t st) {
-  const unsigned grid = (unsigned)(T + E), threads = row_threads(H / 8);
+  const unsigned grid = grid_of(T * k, E);
+  const u32x4 *d = reinterpret_cast<const u32x4*>(dy), *y = reinterpret_cast<const u32x4*>(y_perm);
+  u32x4* const o = reinterpret_cast<u32x4*>(dy_perm);
   if (dprobs)
-    return_bwd_kernel<true><<<grid, threads, 0, st>>>(dy, row_w, H, k, E, row_map, offsets, src_row, M_cap, dy_perm,
-                                                      y_perm, dprobs);
+    return_bwd_kernel<true><<<grid, kThreads, 0, st>>>(d, row_w, H / 8, (int)(T * k), k, E, row_map, offsets, src_row,
+                                                       M_cap, o, y, dprobs);
   else
-    return_bwd_kernel<false><<<grid, threads, 0, st>>>(dy, row_w, H, k, E, row_map, offsets, src_row, M_cap, dy_perm,
-                                                       nullptr, nullptr);
+    return_bwd_kernel<false><<<grid, kThreads, 0, st>>>(d, row_w, H / 8, (int)(T * k), k, E, row_map, offsets, src_row,
+                                                        M_cap, o, nullptr, nullptr);
   return hipGetLastError();
 }
 

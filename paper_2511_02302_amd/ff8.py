@@ -430,8 +430,8 @@ SCORES = {"softmax": 0, "sigmoid": 1}
 
 
 def _here(stream, *tensors):
-    """Every tensor lies on the current device, whose stream the call goes to."""
-    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
+    """Every tensor (checked to be a device tensor) lies on the current device, whose stream the call goes to."""
+    dev = torch._C._cuda_getDevice()
     if stream is not None and stream.device.index != dev:
         raise ValueError(f"the stream is on {stream.device}, the current device is cuda:{dev}")
     for t in tensors:
