@@ -11,6 +11,11 @@
 //   sigmoid             dl_j = c s_j (1 - s_j) dp_j
 //   normalized, r_j     dl_j = c g_j r_j (dp_j - sum_m r_m dp_m),  g = 1 or sigmoid(-l_j)
 // and zero for experts that are not chosen in the last two.
+//
+// What bounds it.  The floor is one read of the logits (8.4 MB at 16384 tokens x 256 experts: about 1.5 us);
+// the work is k rounds of an argmax over the experts, so that is arranged to take few instructions: a token is
+// held by 16 lanes (or by a wave, for few tokens or many experts), its experts in registers, reductions run on
+// DPP and lane swaps instead of LDS, and bf16 logits carry their expert's number in the low half of one word.
 
 #include <math.h>
 
@@ -23,156 +28,327 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ float load_logit(const float* p) { return *p; }
-__device__ __forceinline__ float load_logit(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-__device__ __forceinline__ void store_logit(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_logit(uint16_t* p, float v) { *p = (uint16_t)f32_to_bf16(v); }
+// ---- reductions over the aligned group of L = 16 or 64 lanes (every lane gets the result) ----
 
-__device__ __forceinline__ double max_key(double a, double b) { return a > b ? a : b; }
-__device__ __forceinline__ float max_key(float a, float b) { return a > b ? a : b; }
-
-// Over the aligned group of L lanes (every lane gets the result).
-template <int L, typename V>
-__device__ __forceinline__ V group_max(V v) {
-#pragma unroll
-  for (int d = 1; d < L; d <<= 1) v = max_key(v, __shfl_xor(v, d));
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xF, 0xF, false);
+}
+// f over xor 1, xor 2, half-row mirror and row mirror; then the rows' values by lane swaps.
+template <int L, typename F>
+__device__ __forceinline__ uint32_t group_reduce(uint32_t v, F f) {
+  static_assert(L == 16 || L == 64, "a row of 16 lanes or the wave");
+  v = f(v, dpp<0xB1>(v));
+  v = f(v, dpp<0x4E>(v));
+  v = f(v, dpp<0x141>(v));
+  v = f(v, dpp<0x140>(v));
+  if (L == 64) {
+    auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(r[0], r[1]);
+    r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = f(r[0], r[1]);
+  }
   return v;
 }
 template <int L>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  return group_reduce<L>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int L>
+__device__ __forceinline__ float group_max(float v) {
+  return __uint_as_float(group_reduce<L>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+template <int L>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int d = 1; d < L; d <<= 1) v += __shfl_xor(v, d);
-  return v;
+  return __uint_as_float(group_reduce<L>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
-__device__ __forceinline__ float log_sigmoid(float x) { return fminf(x, 0.0f) - log1pf(expf(-fabsf(x))); }
+// ---- a row's logits: V consecutive experts a lane ----
 
-// L lanes a token, V consecutive experts a lane (L * V >= E), so that among lanes of equal keys the
-// lowest has the lowest expert.  K is the key's type: the logit as it is in float32; score + bias in
-// float64, as a rounding of the sum would decide between experts.
-template <int L, int V, bool kSigmoid, bool kNormalize, typename K, typename X>
-__global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ logits, const float* __restrict__ bias,
-                                                        int64_t T, int E, int k, float scale,
-                                                        int32_t* __restrict__ topk_idx, float* __restrict__ probs) {
-  constexpr bool kBias = sizeof(K) == 8;
-  constexpr int kSlots = L == 64 ? 1 : (64 + L - 1) / L;  // slots a lane holds: k <= 64
-  const int lane = threadIdx.x & (L - 1);
-  const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
-  if (t >= T) return;  // whole groups of L lanes
-  float l[V];
+template <int kBytes>
+struct Piece;
+template <>
+struct Piece<2> { typedef uint16_t type; };
+template <>
+struct Piece<4> { typedef uint32_t type; };
+template <>
+struct Piece<8> { typedef u32x2 type; };
+template <>
+struct Piece<16> { typedef u32x4 type; };
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+__device__ __forceinline__ void from_f32(float* p, float v) { *p = v; }
+__device__ __forceinline__ void from_f32(uint16_t* p, float v) { *p = (uint16_t)f32_to_bf16(v); }
+
+// vec: E is a multiple of V and the tensor is aligned to a lane's piece (at most 16 bytes), so a lane's experts
+// are all there or all missing.
+template <int V, typename X>
+__device__ __forceinline__ void load_row(const X* row, int lane, int E, bool vec, X missing, X (&x)[V]) {
+  constexpr int kBytes = V * sizeof(X) < 16 ? V * sizeof(X) : 16, kPer = kBytes / sizeof(X);
+  typedef typename Piece<kBytes>::type P;
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int i = lane * V + v;
-    l[v] = i < E ? load_logit(logits + t * E + i) : -INFINITY;
-  }
-  float m = -INFINITY, sum = 0.0f;
-  const bool full = !kSigmoid && (kBias || !kNormalize);  // the softmax over all experts is needed
-  if (full) {
+  for (int v = 0; v < V; ++v) x[v] = missing;
+  if (vec) {
+    if (lane * V < E) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) m = fmaxf(m, l[v]);
-    m = group_max<L>(m);
-    if (m == -INFINITY) m = 0.0f;  // no expert can be chosen
-  }
-  K key[V];
-  if (kBias) {
-    double z = 1.0;
-    if (!kSigmoid) {
-      z = 0.0;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        key[v] = exp((double)l[v] - (double)m);
-        z += key[v];
+      for (int v = 0; v < V; v += kPer) {
+        const P p = *reinterpret_cast<const P*>(row + lane * V + v);
+        __builtin_memcpy(&x[v], &p, kBytes);
       }
-#pragma unroll
-      for (int d = 1; d < L; d <<= 1) z += __shfl_xor(z, d);
-      sum = (float)z;
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int i = lane * V + v;
-      const double s = kSigmoid ? 1.0 / (1.0 + exp(-(double)l[v])) : key[v] / z;
-      key[v] = (i < E && l[v] > -INFINITY) ? s + (double)bias[i] : -INFINITY;
     }
   } else {
-    if (full) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) sum += expf(l[v] - m);
-      sum = group_sum<L>(sum);
+    for (int v = 0; v < V; ++v)
+      if (lane * V + v < E) x[v] = row[lane * V + v];
+  }
+}
+template <int V, typename X>
+__device__ __forceinline__ void store_row(X* row, int lane, int E, bool vec, const float (&d)[V]) {
+  constexpr int kBytes = V * sizeof(X) < 16 ? V * sizeof(X) : 16, kPer = kBytes / sizeof(X);
+  typedef typename Piece<kBytes>::type P;
+  X x[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) from_f32(&x[v], d[v]);
+  if (vec) {
+    if (lane * V < E) {
+#pragma unroll
+      for (int v = 0; v < V; v += kPer) {
+        P p;
+        __builtin_memcpy(&p, &x[v], kBytes);
+        *reinterpret_cast<P*>(row + lane * V + v) = p;
+      }
     }
+  } else {
 #pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = l[v];
+    for (int v = 0; v < V; ++v)
+      if (lane * V + v < E) row[lane * V + v] = x[v];
   }
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-    if (!(key[v] > -INFINITY)) key[v] = -INFINITY;  // NaN is never chosen
-  // k rounds: the largest key of the group, the lowest lane that has it, its lowest expert
-  int my_idx[kSlots];
-  float my_l[kSlots];
-#pragma unroll
-  for (int q = 0; q < kSlots; ++q) {
-    my_idx[q] = -1;
-    my_l[q] = -INFINITY;
-  }
+}
+
+// ---- scores ----
+
+// e^d for d <= 0 to about one unit in the last place: the hardware 2^x of the product's head, times
+// 1 + ln 2 * (the product's rounding and log2(e)'s own).  Below e^-200, 0; NaN stays.
+__device__ __forceinline__ float exp_neg(float d) {
+  constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
+  d = d < -200.0f ? -200.0f : d;
+  const float hi = d * kLog2e;
+  const float lo = fmaf(d, kLog2e, -hi) + d * kLog2eLow;
+  const float e = __builtin_amdgcn_exp2f(hi);
+  return fmaf(e, lo * kLn2, e);
+}
+__device__ __forceinline__ float sigmoid(float x) {
+  const float e = exp_neg(-fabsf(x));
+  return (x < 0.0f ? e : 1.0f) / (1.0f + e);
+}
+__device__ __forceinline__ float log_sigmoid(float x) { return fminf(x, 0.0f) - log1pf(exp_neg(-fabsf(x))); }
+
+// Ordered key of a bf16 logit with its expert's number: larger for larger logits, and for lower experts among
+// equal ones; 0 for a logit that is never chosen (-inf, NaN).
+__device__ __forceinline__ uint32_t packed_key(uint16_t b, int i) {
+  const uint32_t u = b == 0x8000 ? 0u : b;
+  const uint32_t ord = u & 0x8000 ? ~u & 0xFFFFu : u | 0x8000u;
+  const bool never = (u & 0x7FFFu) > 0x7F80u || u == 0xFF80u;
+  return never ? 0u : ord << 16 | (0xFFFFu - (uint32_t)i);
+}
+__device__ __forceinline__ float packed_logit(uint32_t key) {
+  const uint32_t ord = key >> 16;
+  return __uint_as_float((ord & 0x8000u ? ord ^ 0x8000u : ~ord & 0xFFFFu) << 16);
+}
+
+// What a round has found, by slot.
+struct Choice {
+  int idx;
+  float logit, key;
+};
+
+// k rounds over keys of type K (-inf: never chosen): the largest of the group, the lowest lane that has it, its
+// lowest expert.  Slot j of `out` is written by the lane that held it; chosen keys become -inf.
+template <int L, int V, typename K>
+__device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], int k, Choice* out) {
+  const int lane = threadIdx.x & (L - 1), base = threadIdx.x & 63 & ~(L - 1);
   for (int j = 0; j < k; ++j) {
     K best = key[0];
 #pragma unroll
-    for (int v = 1; v < V; ++v) best = max_key(best, key[v]);
-    const K top = group_max<L>(best);
-    const unsigned long long who = __ballot(best == top) >> (threadIdx.x & 63 & ~(L - 1));
-    const int win = __ffsll(who) - 1;  // the group's own bits come first
-    int vi = 0;
-    float vl = 0.0f;
-#pragma unroll
-    for (int v = V - 1; v >= 0; --v)
-      if (key[v] == top) {
-        vi = v;
-        vl = l[v];
-      }
-    const bool some = top > -INFINITY;
-    if (some && lane == win) {
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (v == vi) key[v] = -INFINITY;
-    }
-    const int at = (threadIdx.x & 63 & ~(L - 1)) + win;
-    const int ji = some ? win * V + __shfl(vi, at) : -1;
-    const float jl = some ? __shfl(vl, at) : -INFINITY;
-#pragma unroll
-    for (int q = 0; q < kSlots; ++q)
-      if (j == q * L + lane) {
-        my_idx[q] = ji;
-        my_l[q] = jl;
-      }
-  }
-  float vmax = -INFINITY, total = 0.0f;
-  float w[kSlots];
-#pragma unroll
-  for (int q = 0; q < kSlots; ++q) {
-    const int j = q * L + lane;
-    const bool have = j < k && my_idx[q] >= 0;
-    if (kNormalize) {
-      w[q] = have ? (kSigmoid ? log_sigmoid(my_l[q]) : my_l[q]) : -INFINITY;
-      vmax = fmaxf(vmax, w[q]);
+    for (int v = 1; v < V; ++v) best = key[v] > best ? key[v] : best;
+    K top = best;
+    if constexpr (sizeof(K) == 4) {
+      top = group_max<L>(best);
     } else {
-      w[q] = have ? (kSigmoid ? sigmoid(my_l[q]) : expf(my_l[q] - m) / sum) : 0.0f;
+#pragma unroll
+      for (int d = 1; d < L; d <<= 1) {
+        const K o = __shfl_xor(top, d);
+        top = o > top ? o : top;
+      }
     }
+    const int win = __ffsll(__ballot(best == top) >> base) - 1;  // the group's own bits come first
+    bool mine = lane == win;
+    int at = -1;
+    float logit = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const bool hit = mine && key[v] == top;
+      at = hit ? v : at;
+      logit = hit ? l[v] : logit;
+      key[v] = hit ? (K)-INFINITY : key[v];
+      mine = mine && !hit;
+    }
+    if (lane == win) out[j] = {top > -INFINITY ? lane * V + at : -1, logit, (float)top};
   }
+}
+
+template <int L, int V, bool kSigmoid, bool kNormalize, bool kBias, typename X>
+__global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ logits, const float* __restrict__ bias,
+                                                        int64_t T, int E, int k, float scale, bool vec,
+                                                        bool vec_bias, int32_t* __restrict__ topk_idx, float* __restrict__ probs) {
+  constexpr bool kPacked = sizeof(X) == 2 && !kBias;
+  constexpr bool kFull = !kSigmoid && (kBias || !kNormalize);  // the softmax over all experts is needed
+  __shared__ Choice found[kPacked ? 1 : kThreads];             // k <= L slots a group
+  const int lane = threadIdx.x & (L - 1);
+  Choice* const mine = &found[kPacked ? 0 : threadIdx.x & ~(L - 1)];
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+  if (t >= T) return;  // whole groups of L lanes
+  X raw[V], missing;
+  from_f32(&missing, -INFINITY);
+  load_row<V>(logits + t * E, lane, E, vec, missing, raw);
+  float l[V], m = 0.0f, sum = 1.0f, e[kFull ? V : 1];
+#pragma unroll
+  for (int v = 0; v < V; ++v) l[v] = to_f32(raw[v]);
+  if (kFull) {
+    m = l[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) m = fmaxf(m, l[v]);
+    m = group_max<L>(m);
+    if (m == -INFINITY) m = 0.0f;  // no expert can be chosen
+    sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      e[v] = exp_neg(l[v] - m);
+      sum += e[v];
+    }
+    sum = group_sum<L>(sum);
+  }
+  Choice c = {-1, -INFINITY, -INFINITY};
+  if constexpr (kPacked) {
+    uint32_t key[V], word = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = packed_key(raw[v], lane * V + v);
+    for (int j = 0; j < k; ++j) {
+      uint32_t top = key[0];
+#pragma unroll
+      for (int v = 1; v < V; ++v) top = key[v] > top ? key[v] : top;
+      top = group_max<L>(top);
+      word = lane == j ? top : word;
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = key[v] == top ? 0u : key[v];
+    }
+    if (word) c = {(int)(0xFFFFu - (word & 0xFFFFu)), packed_logit(word), 0.0f};
+  } else {
+    float key[V];
+    if (!kBias) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = l[v] > -INFINITY ? l[v] : -INFINITY;  // NaN is never chosen
+      choose_rounds<L, V>(key, l, k, mine);
+    } else {
+      // In float32 first.  Both scores are off by less than 2^-21 (sigmoid: the exponential's and the
+      // reciprocal's unit, damped) or 2^-18 of the row's largest (softmax: a sum of up to 1024), the sum by
+      // half a unit.  A choice is certain where keys that it tells apart are further than twice that from one
+      // another, or come from equal logits and biases; any other row is decided in float64.
+      const float inv = 1.0f / sum;
+      float b[V];
+      load_row<V>(bias, lane, E, vec_bias, 0.0f, b);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float s = kSigmoid ? __builtin_amdgcn_rcpf(1.0f + __expf(-l[v])) : e[kFull ? v : 0] * inv;
+        const float sum_b = s + b[v];
+        key[v] = ((l[v] > -INFINITY) & (sum_b > -INFINITY)) ? sum_b : -INFINITY;
+      }
+      choose_rounds<L, V>(key, l, k, mine);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const float err = kSigmoid ? 0x1p-19f : 0x1p-16f * inv;
+      bool unsure = false;
+      if (lane + 1 < k) {
+        const Choice a = mine[lane], n = mine[lane + 1];
+        if (n.idx >= 0 && !(a.key - n.key > err + 0x1p-21f * fabsf(a.key)))
+          unsure = !(a.logit == n.logit && bias[a.idx] == bias[n.idx]);
+      }
+      const Choice last = mine[k - 1];
+      if (last.idx >= 0) {
+        const float lb = bias[last.idx], near = last.key - (err + 0x1p-21f * fabsf(last.key));
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          unsure |= (key[v] > -INFINITY) & !(key[v] < near) & !((l[v] == last.logit) & (b[v] == lb));
+      }
+      if (__any(unsure)) {
+        double z = 1.0, key64[V];
+        if (!kSigmoid) {
+          z = 0.0;
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            key64[v] = exp((double)l[v] - (double)m);
+            z += key64[v];
+          }
+#pragma unroll
+          for (int d = 1; d < L; d <<= 1) z += __shfl_xor(z, d);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const double s = kSigmoid ? 1.0 / (1.0 + exp(-(double)l[v])) : key64[v] / z;
+          const double sum_b = s + (double)b[v];
+          key64[v] = ((l[v] > -INFINITY) & (sum_b > -INFINITY)) ? sum_b : -INFINITY;  // a missing expert's l is -inf
+        }
+        choose_rounds<L, V>(key64, l, k, mine);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (lane < k) c = mine[lane];
+  }
+  float w = 0.0f;
   if (kNormalize) {
-    vmax = group_max<L>(vmax);
-#pragma unroll
-    for (int q = 0; q < kSlots; ++q) {
-      w[q] = w[q] > -INFINITY ? expf(w[q] - vmax) : 0.0f;
-      total += w[q];
-    }
-    total = group_sum<L>(total);
+    w = c.idx >= 0 ? (kSigmoid ? log_sigmoid(c.logit) : c.logit) : -INFINITY;
+    const float top = group_max<L>(w);
+    w = w > -INFINITY ? exp_neg(w - top) : 0.0f;
+    w = w / group_sum<L>(w);
+  } else {
+    w = kSigmoid ? sigmoid(c.logit) : exp_neg(c.logit - m) / sum;
   }
+  if (lane < k) {
+    topk_idx[t * k + lane] = c.idx;
+    probs[t * k + lane] = c.idx < 0 ? 0.0f : scale * w;
+  }
+}
+
+// d[v] += g of every slot whose expert is the lane's v-th; slots in order, so that the sum of an expert that is
+// there twice has one order.
+template <int L, int V, int J>
+__device__ __forceinline__ void spread_slot(int idx, float g, int k, int lane, float (&d)[V]) {
+  if constexpr (J < 16) {
+    if (J >= k) return;  // uniform
+    // lane J of the row to all its lanes
+    const int at = (int)dpp<0x150 + J>((uint32_t)idx) - lane * V;
+    const float gj = __uint_as_float(dpp<0x150 + J>(__float_as_uint(g)));
 #pragma unroll
-  for (int q = 0; q < kSlots; ++q) {
-    const int j = q * L + lane;
-    if (j < k) {
-      topk_idx[t * k + j] = my_idx[q];
-      probs[t * k + j] = my_idx[q] < 0 ? 0.0f : scale * (kNormalize ? w[q] / total : w[q]);
+    for (int v = 0; v < V; ++v) d[v] += at == v ? gj : 0.0f;
+    spread_slot<L, V, J + 1>(idx, g, k, lane, d);
+  }
+}
+template <int L, int V>
+__device__ __forceinline__ void spread(int idx, float g, int k, int lane, float (&d)[V]) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) d[v] = 0.0f;
+  if constexpr (L == 16) {
+    spread_slot<L, V, 0>(idx, g, k, lane, d);
+  } else {
+    for (int j = 0; j < k; ++j) {
+      const int at = __builtin_amdgcn_readlane(idx, j) - lane * V;
+      const float gj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), j));
+#pragma unroll
+      for (int v = 0; v < V; ++v) d[v] += at == v ? gj : 0.0f;
     }
   }
 }
@@ -181,105 +357,105 @@ template <int L, int V, bool kSigmoid, bool kNormalize, typename X>
 __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict__ logits,
                                                             const int32_t* __restrict__ topk_idx,
                                                             const float* __restrict__ dprobs, int64_t T, int E, int k,
-                                                            float scale, X* __restrict__ dlogits) {
-  constexpr int kSlots = L == 64 ? 1 : (64 + L - 1) / L;
+                                                            float scale, bool vec, X* __restrict__ dlogits) {
+  constexpr bool kDense = !kSigmoid && !kNormalize;
   const int lane = threadIdx.x & (L - 1);
   const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
   if (t >= T) return;
   const X* row = logits + t * E;
-  // the chosen: index, logit and weight's gradient, slot q * L + lane
-  int idx[kSlots];
-  float cl[kSlots], g[kSlots];
-#pragma unroll
-  for (int q = 0; q < kSlots; ++q) {
-    const int j = q * L + lane;
-    idx[q] = j < k ? topk_idx[t * k + j] : -1;
-    if (idx[q] >= E) idx[q] = -1;
-    cl[q] = idx[q] >= 0 ? load_logit(row + idx[q]) : -INFINITY;
-    g[q] = idx[q] >= 0 ? dprobs[t * k + j] : 0.0f;
-  }
-  const bool dense = !kSigmoid && !kNormalize;
-  float l[V], m = -INFINITY, sum = 0.0f, dot = 0.0f;
-  if (dense) {
+  float d[V];
+  // slot `lane`: its expert (-1: none) and its weight's gradient
+  int idx = lane < k ? topk_idx[t * k + lane] : -1;
+  if (idx >= E) idx = -1;
+  float g = lane < k ? dprobs[t * k + lane] : 0.0f;
+  if (idx < 0) g = 0.0f;
+  if (kDense) {
+    X raw[V], missing;
+    from_f32(&missing, -INFINITY);
+    load_row<V>(row, lane, E, vec, missing, raw);
+    float p[V], m = -INFINITY, sum = 0.0f, dot = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int i = lane * V + v;
-      l[v] = i < E ? load_logit(row + i) : -INFINITY;
-      m = fmaxf(m, l[v]);
+      p[v] = to_f32(raw[v]);
+      m = fmaxf(m, p[v]);
     }
     m = group_max<L>(m);
     if (m == -INFINITY) m = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      l[v] = expf(l[v] - m);
-      sum += l[v];
+      p[v] = exp_neg(p[v] - m);
+      sum += p[v];
     }
     sum = group_sum<L>(sum);
-    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    spread<L, V>(idx, g, k, lane, d);
 #pragma unroll
-    for (int v = 0; v < V; ++v) l[v] *= inv;
-#pragma unroll
-    for (int q = 0; q < kSlots; ++q)
-      if (idx[q] >= 0) dot += expf(cl[q] - m) * inv * g[q];
-    dot = group_sum<L>(dot);
-  } else if (kNormalize) {
-    float vmax = -INFINITY, total = 0.0f, r[kSlots];
-#pragma unroll
-    for (int q = 0; q < kSlots; ++q) {
-      r[q] = idx[q] >= 0 ? (kSigmoid ? log_sigmoid(cl[q]) : cl[q]) : -INFINITY;
-      vmax = fmaxf(vmax, r[q]);
-    }
-    vmax = group_max<L>(vmax);
-#pragma unroll
-    for (int q = 0; q < kSlots; ++q) {
-      r[q] = r[q] > -INFINITY ? expf(r[q] - vmax) : 0.0f;
-      total += r[q];
-    }
-    total = group_sum<L>(total);
-#pragma unroll
-    for (int q = 0; q < kSlots; ++q) {
-      r[q] = total > 0.0f || total != total ? r[q] / total : 0.0f;
-      dot += r[q] * g[q];
+    for (int v = 0; v < V; ++v) {
+      p[v] *= inv;
+      dot = fmaf(p[v], d[v], dot);
     }
     dot = group_sum<L>(dot);
 #pragma unroll
-    for (int q = 0; q < kSlots; ++q) g[q] = scale * r[q] * (g[q] - dot) * (kSigmoid ? sigmoid(-cl[q]) : 1.0f);
+    for (int v = 0; v < V; ++v) d[v] = scale * p[v] * (d[v] - dot);
   } else {
-#pragma unroll
-    for (int q = 0; q < kSlots; ++q) {
-      g[q] = idx[q] >= 0 ? scale * g[q] * sigmoid(cl[q]) * sigmoid(-cl[q]) : 0.0f;
+    const float l = idx >= 0 ? to_f32(row[idx]) : -INFINITY;
+    if (kNormalize) {
+      float r = idx >= 0 ? (kSigmoid ? log_sigmoid(l) : l) : -INFINITY;
+      const float top = group_max<L>(r);
+      r = r > -INFINITY ? exp_neg(r - top) : 0.0f;
+      const float total = group_sum<L>(r);
+      r = total == 0.0f ? 0.0f : r / total;
+      const float dot = group_sum<L>(r * g);
+      g = scale * r * (g - dot) * (kSigmoid ? sigmoid(-l) : 1.0f);
+    } else if (idx >= 0) {
+      g = scale * g * sigmoid(l) * sigmoid(-l);
     }
+    spread<L, V>(idx, g, k, lane, d);
   }
-  float d[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) d[v] = 0.0f;
-  const int base = threadIdx.x & 63 & ~(L - 1);
-#pragma unroll
-  for (int q = 0; q < kSlots; ++q) {
-    const int n = k - q * L < L ? k - q * L : L;
-    for (int j = 0; j < n; ++j) {
-      const int at = __shfl(idx[q], base + j) - lane * V;  // of an index of -1 below zero for every lane
-      const float gj = __shfl(g[q], base + j);
-#pragma unroll
-      for (int v = 0; v < V; ++v) d[v] += at == v ? gj : 0.0f;
-    }
-  }
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int i = lane * V + v;
-    if (i < E) store_logit(dlogits + t * E + i, dense ? scale * l[v] * (d[v] - dot) : d[v]);
-  }
+  store_row<V>(dlogits + t * E, lane, E, vec, d);
+}
+
+// Lanes a token.  Sixteen (four tokens a wave) take a quarter of the reductions of a whole wave but hold four
+// times the experts a lane: the wave is for few tokens, where a round's latency counts, for k above 16 (a
+// lane holds a slot) and for more than 256 experts.
+int lanes_of(int64_t T, int E, int k) {
+  if (E > 256 || k > 16) return 64;
+  return E > 64 && T <= 2048 ? 64 : 16;
+}
+
+// CALL(lanes, experts a lane)
+#define FF8_BY_SIZE(T, E, k, CALL)          \
+  if (lanes_of(T, E, k) == 16) {            \
+    if ((E) <= 16) return CALL(16, 1);      \
+    if ((E) <= 32) return CALL(16, 2);      \
+    if ((E) <= 64) return CALL(16, 4);      \
+    if ((E) <= 128) return CALL(16, 8);     \
+    return CALL(16, 16);                    \
+  }                                         \
+  if ((E) <= 64) return CALL(64, 1);        \
+  if ((E) <= 128) return CALL(64, 2);       \
+  if ((E) <= 256) return CALL(64, 4);       \
+  if ((E) <= 512) return CALL(64, 8);       \
+  return CALL(64, 16);
+
+template <int V, typename X>
+bool vector_rows(int E, const void* a, const void* b) {
+  constexpr uintptr_t kBytes = V * sizeof(X) < 16 ? V * sizeof(X) : 16;
+  return E % V == 0 && (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % kBytes == 0;
 }
 
 template <int L, int V, typename X>
 hipError_t topk_launch(const X* logits, const float* bias, int64_t T, int E, int k, bool sig, bool norm, float scale,
                        int32_t* idx, float* probs, hipStream_t st) {
   const unsigned grid = (unsigned)((T + kThreads / L - 1) / (kThreads / L));
-#define FF8_GO(S, N)                                                                                             \
-  if (bias)                                                                                                      \
-    topk_kernel<L, V, S, N, double, X><<<grid, kThreads, 0, st>>>(logits, bias, T, E, k, scale, idx, probs);     \
-  else                                                                                                           \
-    topk_kernel<L, V, S, N, float, X><<<grid, kThreads, 0, st>>>(logits, bias, T, E, k, scale, idx, probs);
+  const bool vec = vector_rows<V, X>(E, logits, nullptr), vec_bias = vector_rows<V, float>(E, bias, nullptr);
+#define FF8_GO(S, N)                                                                                               \
+  if (bias)                                                                                                        \
+    topk_kernel<L, V, S, N, true, X><<<grid, kThreads, 0, st>>>(logits, bias, T, E, k, scale, vec, vec_bias, idx,  \
+                                                                probs);                                            \
+  else                                                                                                             \
+    topk_kernel<L, V, S, N, false, X><<<grid, kThreads, 0, st>>>(logits, bias, T, E, k, scale, vec, false, idx,    \
+                                                                 probs);
   if (sig && norm) {
     FF8_GO(true, true)
   } else if (sig) {
@@ -297,8 +473,9 @@ template <int L, int V, typename X>
 hipError_t topk_bwd_launch(const X* logits, const int32_t* idx, const float* dprobs, int64_t T, int E, int k, bool sig,
                            bool norm, float scale, X* dlogits, hipStream_t st) {
   const unsigned grid = (unsigned)((T + kThreads / L - 1) / (kThreads / L));
+  const bool vec = vector_rows<V, X>(E, logits, dlogits);
 #define FF8_GO(S, N) \
-  topk_bwd_kernel<L, V, S, N, X><<<grid, kThreads, 0, st>>>(logits, idx, dprobs, T, E, k, scale, dlogits)
+  topk_bwd_kernel<L, V, S, N, X><<<grid, kThreads, 0, st>>>(logits, idx, dprobs, T, E, k, scale, vec, dlogits)
   if (sig && norm)
     FF8_GO(true, true);
   else if (sig)
@@ -311,22 +488,12 @@ hipError_t topk_bwd_launch(const X* logits, const int32_t* idx, const float* dpr
   return hipGetLastError();
 }
 
-// Lanes and experts a lane by E: 16 lanes (four tokens a wave) up to 256 experts, the whole wave above.
-#define FF8_BY_E(E, CALL)                  \
-  if ((E) <= 16) return CALL(16, 1);       \
-  if ((E) <= 32) return CALL(16, 2);       \
-  if ((E) <= 64) return CALL(16, 4);       \
-  if ((E) <= 128) return CALL(16, 8);      \
-  if ((E) <= 256) return CALL(16, 16);     \
-  if ((E) <= 512) return CALL(64, 8);      \
-  return CALL(64, 16);
-
 template <typename X>
 hipError_t topk_impl(const X* logits, const float* bias, int64_t T, int E, int k, bool sig, bool norm, float scale,
                      int32_t* idx, float* probs, hipStream_t st) {
   if (T == 0) return hipSuccess;
 #define FF8_CALL(L, V) topk_launch<L, V, X>(logits, bias, T, E, k, sig, norm, scale, idx, probs, st)
-  FF8_BY_E(E, FF8_CALL)
+  FF8_BY_SIZE(T, E, k, FF8_CALL)
 #undef FF8_CALL
 }
 
@@ -335,7 +502,7 @@ hipError_t topk_bwd_impl(const X* logits, const int32_t* idx, const float* dprob
                          bool norm, float scale, X* dlogits, hipStream_t st) {
   if (T == 0) return hipSuccess;
 #define FF8_CALL(L, V) topk_bwd_launch<L, V, X>(logits, idx, dprobs, T, E, k, sig, norm, scale, dlogits, st)
-  FF8_BY_E(E, FF8_CALL)
+  FF8_BY_SIZE(T, E, k, FF8_CALL)
 #undef FF8_CALL
 }
 
