@@ -75,6 +75,8 @@ __global__ __launch_bounds__(kThreads) void pack_mxfp4_kernel(const uint8_t* __r
   ts[i] = s[row * k_tiles * 4 + piece];
 }
 
+__device__ __forceinline__ float swiglu(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+
 // 8 codes (one dword) times 2^T as bf16.
 __device__ __forceinline__ bf16x8_t decode8(uint32_t w, float scale) {
   const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
@@ -84,17 +86,178 @@ __device__ __forceinline__ bf16x8_t decode8(uint32_t w, float scale) {
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Which 16 rows of which expert block number mb is; e < 0 behind the last.  Every wave finds it by
-// itself: 64 experts at a time, a scan of their counts of blocks.
+// What a wave computes at a time: kTiles tiles of 16 weight rows (with kSwiglu half of them gate rows and half the
+// up rows beside them).  D = weights (16 x 32) times tokens^T (32 x 16): lane l holds token l % 16, weight rows
+// 4 (l / 16) .. + 3 of a tile.  The weights' tiles are read with column block s of their expert.
+constexpr int kTiles = 4;
+template <bool kSwiglu>
+__device__ __forceinline__ void weight_tiles(int e, int64_t n0, int64_t N, int64_t kt, int64_t (&tile)[kTiles]) {
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    const int64_t n = kSwiglu ? (i < kTiles / 2 ? n0 + 16 * i : N / 2 + n0 + 16 * (i - kTiles / 2)) : n0 + 16 * i;
+    tile[i] = ((int64_t)e * N + n) / 16 * kt;
+  }
+}
+__device__ __forceinline__ void fetch_weights(const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts,
+                                              const int64_t (&tile)[kTiles], int64_t s, u32x4 (&w)[kTiles],
+                                              uint32_t (&sc)[kTiles]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    w[i] = ldnt16(tq + (tile[i] + s) * 1024 + lane * 16);
+    sc[i] = __builtin_nontemporal_load(ts + (tile[i] + s) * 64 + lane);
+  }
+}
+// The wave's number, as a value that the compiler knows to be the same in all lanes: what depends on it alone is
+// computed once, in scalar registers.
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+// Loads before this point are issued before it and later ones after it: waits count loads in their order.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// The source row of a grouped row, -1 for padding (and for source rows out of range).
+__device__ __forceinline__ int source_of(int64_t row, const int32_t* __restrict__ src_row, int top_k, int64_t x_rows) {
+  if (!src_row) return (int)row;
+  const int src = src_row[row];
+  if (src < 0) return -1;
+  if (top_k == 0) return (int)row;
+  return src / top_k < x_rows ? src / top_k : -1;
+}
+
+// A lane's 16-byte piece p of row r of a 128-column block of x in LDS: pieces are exchanged within a row by the
+// row's number, so that 16 lanes that read one piece of 16 rows meet 16 different places (256-byte rows would put
+// them into the same banks).
+__device__ __forceinline__ int x_place(int r, int p) { return r * 16 + (p ^ (r & 15)); }
+
+// ---- few rows per expert ----
+// A workgroup computes 64 weight rows for 16 token rows of one expert.  Its waves share the column blocks (wave w
+// takes blocks w, w + kWaves, ...), so that nothing but the end needs the other waves: their float32 sums meet in
+// LDS and are added in wave order.  Groups are multiples of 16 rows, so block b is rows 16 b .. + 15 and only its
+// expert has to be looked up.  A wave brings its own piece of x through LDS into the order of the matrix
+// instruction; in registers it has two blocks of weights and x in flight.
+template <bool kSwiglu, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
+    const uint16_t* __restrict__ x, int64_t x_rows, const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts,
+    const int32_t* __restrict__ offsets, int E, const int32_t* __restrict__ src_row, int top_k, int64_t N, int64_t K,
+    uint16_t* __restrict__ out) {
+  __shared__ float part[kWaves][kTiles * 256];  // also x, a block a wave
+  const int lane = threadIdx.x & 63, wave = wave_number();
+  constexpr int kCols = kSwiglu ? kTiles * 8 : kTiles * 16;  // columns of out that a workgroup writes
+  const int64_t n_out = kSwiglu ? N / 2 : N, kt = K / kTile;
+  const unsigned nt = (unsigned)(n_out / kCols), mb = blockIdx.x / nt;
+  const int64_t n0 = (int64_t)(blockIdx.x - mb * nt) * kCols, row0 = (int64_t)mb * 16;
+  const int src = source_of(row0 + (lane & 15), src_row, top_k, x_rows);  // rows below M_cap; used below offsets[E]
+  int e = -1;
+  for (int e0 = 0; e0 < E && e < 0; e0 += 64) {
+    const int i = e0 + lane;
+    const bool here = i < E && offsets[i] <= row0 && row0 < offsets[i + 1];
+    const unsigned long long m = __ballot(here);
+    if (m) e = e0 + __ffsll(m) - 1;
+  }
+  if (e < 0) return;  // behind the last group; the same for the whole workgroup
+  const unsigned mask = (unsigned)__ballot(src >= 0) & 0xFFFFu;
+  if (mask) {
+    // the rows a lane brings: row 4 i + lane / 16, piece lane % 16 of a block; padding rows read one that is read anyway
+    const int first = __ffs(mask) - 1;
+    const u32x4* xp[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int q = 4 * i + (lane >> 4);
+      xp[i] = reinterpret_cast<const u32x4*>(x + (int64_t)__shfl(src, mask >> q & 1 ? q : first) * K) + (lane & 15);
+    }
+    u32x4* const xs = reinterpret_cast<u32x4*>(&part[wave][0]);
+    int64_t tile[kTiles];
+    weight_tiles<kSwiglu>(e, n0, N, kt, tile);
+    f32x4 acc[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    u32x4 wb[2][kTiles], xb[2][4];
+    uint32_t sb[2][kTiles];
+    auto fetch = [&](int64_t s, int d) {
+      keep_order();
+      fetch_weights(tq, ts, tile, s, wb[d], sb[d]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xb[d][i] = xp[i][s * 16];
+      keep_order();
+    };
+    auto step = [&](int d) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xs[x_place(4 * i + (lane >> 4), lane & 15)] = xb[d][i];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8_t b = __builtin_bit_cast(bf16x8_t, xs[x_place(lane & 15, (lane >> 4) * 4 + j)]);
+        bf16x8_t a[kTiles];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) a[i] = decode8(wb[d][i][j], __uint_as_float(sb[d][i] << 23));
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b, acc[i], 0, 0, 0);
+        keep_order();  // decoding all of the block first would take 64 more registers
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    // Two blocks in flight.  No load is behind a condition, so that the waits in front of a step count the loads
+    // behind it and leave them in flight; behind its last block a wave loads that one again.
+    const int64_t n = (kt - wave + kWaves - 1) / kWaves;
+    auto block = [&](int64_t i) { return wave + (i < n ? i : n - 1) * kWaves; };
+    if (n > 0) {
+      fetch(block(0), 0);
+      fetch(block(1), 1);
+      for (int64_t i = 0; i < n; i += 2) {
+        step(0);
+        fetch(block(i + 2), 0);
+        if (i + 1 == n) break;
+        step(1);
+        fetch(block(i + 3), 1);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) *reinterpret_cast<f32x4*>(&part[wave][i * 256 + lane * 4]) = acc[i];
+  }
+  __syncthreads();
+  // elements q, q + 1: tile q / 256, token (q / 4) % 16, weight rows 4 ((q / 64) % 4) + q % 4 .. + 1 of the tile
+  for (int q = 2 * threadIdx.x; q < kCols * 16; q += kWaves * 128) {
+    const int token = (q >> 2) & 15, n = (q >> 8) * 16 + ((q >> 6) & 3) * 4 + (q & 3);
+    f32x2 v = {0.0f, 0.0f};
+    if (mask >> token & 1) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const f32x2 p = *reinterpret_cast<const f32x2*>(&part[w][q]);
+        v[0] += p[0];
+        v[1] += p[1];
+      }
+      if (kSwiglu) {
+        f32x2 u = {0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const f32x2 p = *reinterpret_cast<const f32x2*>(&part[w][q + kTiles * 128]);
+          u[0] += p[0];
+          u[1] += p[1];
+        }
+        v[0] = swiglu(v[0], u[0]);
+        v[1] = swiglu(v[1], u[1]);
+      }
+    }
+    *reinterpret_cast<uint32_t*>(out + (row0 + token) * n_out + n0 + n) = pack_bf16x2(v[0], v[1]);
+  }
+}
+
+// ---- many rows per expert ----
+// A workgroup of four waves computes 256 weight rows (64 a wave) for up to 96 token rows of one expert: every
+// wave goes through all column blocks and shares the block of x, which the workgroup brings into one of two LDS
+// buffers while it computes from the other.
+constexpr int kManyWaves = 4, kManyThreads = 64 * kManyWaves, kManyRows = 96;
+
+// Rows of block mb: its expert (-1 behind the last), first row and number of rows, a multiple of 16.  An expert's
+// rows are split evenly over the fewest blocks of at most 96.
 struct RowBlock {
   int e, row, n;
 };
-__device__ __forceinline__ RowBlock find_block(int64_t mb, const int32_t* __restrict__ offsets, int E) {
+__device__ __forceinline__ RowBlock find_block(int mb, const int32_t* __restrict__ offsets, int E) {
   const int lane = threadIdx.x & 63;
   for (int e0 = 0; e0 < E; e0 += 64) {
-    const int e = e0 + lane;
-    const int g0 = e < E ? offsets[e] : 0, g1 = e < E ? offsets[e + 1] : 0;
-    const int nb = (g1 - g0 + 15) / 16;
+    const int i = e0 + lane;
+    const int g0 = i < E ? offsets[i] : 0, g = i < E ? offsets[i + 1] - g0 : 0;
+    const int nb = (g + kManyRows - 1) / kManyRows;
     int end = nb;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -103,115 +266,154 @@ __device__ __forceinline__ RowBlock find_block(int64_t mb, const int32_t* __rest
     }
     const int total = __shfl(end, 63);
     if (mb < total) {
-      const int at = __ffsll(__ballot((int64_t)end > mb)) - 1;
-      const int row = __shfl(g0, at) + 16 * ((int)mb - __shfl(end - nb, at));
-      const int left = __shfl(g1, at) - row;
-      return {e0 + at, row, left < 16 ? left : 16};
+      const int at = __ffsll(__ballot(end > mb)) - 1;
+      const int b = mb - __shfl(end - nb, at), n = __shfl(g, at), n_b = __shfl(nb, at);
+      const int per = ((n / 16 + n_b - 1) / n_b) * 16, left = n - b * per;
+      return {e0 + at, __shfl(g0, at) + b * per, left < per ? left : per};
     }
     mb -= total;
   }
   return {-1, 0, 0};
 }
 
-// A workgroup computes 64 weight rows (with kSwiglu 32 gate rows and the 32 up rows beside them) for 16
-// token rows of one expert: four tiles of 16 weight rows, which its eight waves share by column blocks
-// (wave w takes blocks w, w + 8, ...), so that nothing but the end needs the other waves: their float32
-// sums meet in LDS and are added in wave order.  D = weights (16 x 32) times tokens^T (32 x 16): lane l
-// holds token l % 16, weight rows 4 (l / 16) .. + 3 of a tile.
-constexpr int kWaves = 8, kTiles = 4, kDepth = 2;
+// The products of one workgroup with kM x 16 token rows.
+template <bool kSwiglu, int kM>
+__device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const int* __restrict__ rows,
+                                          const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts, int e,
+                                          int64_t n0, int64_t N, int64_t K, bool active,
+                                          const RowBlock& blk,
+                                          const unsigned long long (&real)[2], u32x4* xs,
+                                          uint16_t* __restrict__ out) {
+  const int lane = threadIdx.x & 63, t16 = threadIdx.x >> 4, piece = threadIdx.x & 15;
+  const int64_t kt = K / kTile, n_out = kSwiglu ? N / 2 : N;
+  const u32x4* xp[kM];
+#pragma unroll
+  for (int m = 0; m < kM; ++m) xp[m] = reinterpret_cast<const u32x4*>(x + (int64_t)rows[16 * m + t16] * K) + piece;
+  int64_t tile[kTiles];
+  weight_tiles<kSwiglu>(e, n0, N, kt, tile);
+  f32x4 acc[kTiles][kM];
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+    for (int m = 0; m < kM; ++m) acc[i][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  u32x4 wb[2][kTiles], xb[kM];
+  uint32_t sb[2][kTiles];
+#pragma unroll
+  for (int m = 0; m < kM; ++m) xb[m] = xp[m][0];
+  keep_order();
+  fetch_weights(tq, ts, tile, 0, wb[0], sb[0]);
+  keep_order();
+  fetch_weights(tq, ts, tile, kt > 1 ? 1 : 0, wb[1], sb[1]);
+  keep_order();
+#pragma unroll
+  for (int m = 0; m < kM; ++m) xs[x_place(16 * m + t16, piece)] = xb[m];
+  __syncthreads();
+  for (int64_t s = 0; s < kt; s += 2) {
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const int64_t now = s + d;
+      if (now >= kt) break;  // uniform
+      // no load is behind a condition, so that the waits count the loads behind them; the last blocks load again
+      const int64_t x_next = now + 1 < kt ? now + 1 : now, w_next = now + 2 < kt ? now + 2 : kt - 1;
+#pragma unroll
+      for (int m = 0; m < kM; ++m) xb[m] = xp[m][x_next * 16];
+      keep_order();
+      {
+        const u32x4* const xd = xs + d * kManyRows * 16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          bf16x8_t a[kTiles];
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) a[i] = decode8(wb[d][i][j], __uint_as_float(sb[d][i] << 23));
+#pragma unroll
+          for (int m = 0; m < kM; ++m) {
+            const bf16x8_t b =
+                __builtin_bit_cast(bf16x8_t, xd[x_place(16 * m + (lane & 15), (lane >> 4) * 4 + j)]);
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+              acc[i][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b, acc[i][m], 0, 0, 0);
+          }
+        }
+        keep_order();
+        fetch_weights(tq, ts, tile, w_next, wb[d], sb[d]);
+        keep_order();
+      }
+#pragma unroll
+      for (int m = 0; m < kM; ++m) xs[(1 - d) * kManyRows * 16 + x_place(16 * m + t16, piece)] = xb[m];
+      __syncthreads();
+    }
+  }
+  if (!active) return;
+#pragma unroll
+  for (int m = 0; m < kM; ++m) {
+    const int token = 16 * m + (lane & 15);
+    if (token >= blk.n) continue;
+    const bool ok = real[token >> 6] >> (token & 63) & 1;
+    uint16_t* const o = out + (int64_t)(blk.row + token) * n_out + n0 + (lane >> 4) * 4;
+#pragma unroll
+    for (int i = 0; i < (kSwiglu ? kTiles / 2 : kTiles); ++i) {
+      f32x4 v = acc[i][m];
+      if (kSwiglu) {
+#pragma unroll
+        for (int z = 0; z < 4; ++z) v[z] = swiglu(v[z], acc[i + kTiles / 2][m][z]);
+      }
+      const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      st8(o + 16 * i, ok ? w : u32x2{0u, 0u});
+    }
+  }
+}
+
 template <bool kSwiglu>
-__global__ __launch_bounds__(kWaves * 64) void gemv_mxfp4_kernel(
+__global__ __launch_bounds__(kManyThreads, 2) void gemm_mxfp4_kernel(
     const uint16_t* __restrict__ x, int64_t x_rows, const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts,
     const int32_t* __restrict__ offsets, int E, const int32_t* __restrict__ src_row, int top_k, int64_t M_cap,
     int64_t N, int64_t K, uint16_t* __restrict__ out) {
-  __shared__ float part[kWaves][kTiles * 256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n_cols = kSwiglu ? kTiles * 8 : kTiles * 16;  // columns of out that a workgroup writes
+  __shared__ u32x4 xs[2 * kManyRows * 16];
+  __shared__ int rows[kManyRows];
+  constexpr int kCols = kSwiglu ? kTiles * 8 : kTiles * 16;  // of out, a wave
   const int64_t n_out = kSwiglu ? N / 2 : N;
-  const int64_t nt = n_out / n_cols, kt = K / kTile;
-  for (int64_t item = blockIdx.x;; item += gridDim.x) {
-    const int64_t mb = item / nt, n0 = (item - mb * nt) * n_cols;
-    const RowBlock b = find_block(mb, offsets, E);
-    if (b.e < 0 || b.row + b.n > M_cap) return;  // uniform
-    // the rows' inputs; padding rows (and source rows out of range) give zeros and read nothing of x
-    const int c = lane & 15;
-    int64_t xr = b.row + c;
-    bool real = c < b.n;
-    if (real && src_row) {
-      const int src = src_row[b.row + c];
-      real = src >= 0;
-      if (top_k) {
-        xr = src / top_k;
-        real = real && xr < x_rows;
-      }
-    }
-    const unsigned mask = (unsigned)__ballot(real) & 0xFFFFu;
-    if (mask) {
-      xr = __shfl((int)xr, real ? lane : __ffs(mask) - 1);  // others read a row that is read anyway
-      const uint16_t* const xp = x + xr * K + (lane >> 4) * 32;
-      int64_t tile[kTiles];
+  const unsigned nt = (unsigned)((n_out + kManyWaves * kCols - 1) / (kManyWaves * kCols)), mb = blockIdx.x / nt;
+  const RowBlock blk = find_block((int)mb, offsets, E);
+  if (blk.e < 0 || blk.row + blk.n > M_cap) return;  // uniform
+  const int lane = threadIdx.x & 63;
+  int64_t n0 = ((int64_t)(blockIdx.x - mb * nt) * kManyWaves + wave_number()) * kCols;
+  const bool active = n0 < n_out;  // not so for waves of the last workgroup where n_out is no multiple of its columns:
+  if (!active) n0 = 0;             // they go along and store nothing
+  unsigned long long real[2];
+  int src[2];
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        const int64_t n = kSwiglu ? (i < kTiles / 2 ? n0 + 16 * i : n_out + n0 + 16 * (i - kTiles / 2)) : n0 + 16 * i;
-        tile[i] = (((int64_t)b.e * N + n) / 16) * kt;
-      }
-      f32x4 acc[kTiles];
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      u32x4 wb[kDepth][kTiles], xb[kDepth][4];
-      uint32_t sb[kDepth][kTiles];
-      auto fetch = [&](int64_t s, int d) {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          wb[d][i] = ldnt16(tq + (tile[i] + s) * 1024 + lane * 16);
-          sb[d][i] = ts[(tile[i] + s) * 64 + lane];
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) xb[d][j] = ld16(xp + s * kTile + 8 * j);
-      };
-#pragma unroll
-      for (int d = 0; d < kDepth; ++d)
-        if (wave + d * kWaves < kt) fetch(wave + d * kWaves, d);
-      for (int64_t s = wave; s < kt; s += kDepth * kWaves) {
-#pragma unroll
-        for (int d = 0; d < kDepth; ++d) {
-          const int64_t now = s + d * kWaves;
-          if (now >= kt) break;
-#pragma unroll
-          for (int i = 0; i < kTiles; ++i) {
-            const float scale = __uint_as_float(sb[d][i] << 23);  // the hardware reads the exponent byte alone
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(wb[d][i][j], scale),
-                                                               __builtin_bit_cast(bf16x8_t, xb[d][j]), acc[i], 0, 0, 0);
-          }
-          if (now + kDepth * kWaves < kt) fetch(now + kDepth * kWaves, d);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) *reinterpret_cast<f32x4*>(&part[wave][i * 256 + lane * 4]) = acc[i];
-    }
-    __syncthreads();
-    // element q: tile q / 256, token (q / 4) % 16, weight row 4 ((q / 64) % 4) + q % 4 of the tile
-    for (int q = threadIdx.x; q < (kSwiglu ? kTiles / 2 : kTiles) * 256; q += kWaves * 64) {
-      const int token = (q >> 2) & 15, n = (q >> 8) * 16 + ((q >> 6) & 3) * 4 + (q & 3);
-      if (token >= b.n) continue;
-      float v = 0.0f;
-      if (mask >> token & 1) {
-        v = part[0][q];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) v += part[w][q];
-        if (kSwiglu) {
-          float u = part[0][q + kTiles * 128];
-#pragma unroll
-          for (int w = 1; w < kWaves; ++w) u += part[w][q + kTiles * 128];
-          v = v / (1.0f + expf(-v)) * u;
-        }
-      }
-      out[(b.row + token) * n_out + n0 + n] = (uint16_t)f32_to_bf16(v);
-    }
-    __syncthreads();
+  for (int h = 0; h < 2; ++h) {
+    const int r = 64 * h + lane;
+    src[h] = r < blk.n ? source_of(blk.row + r, src_row, top_k, x_rows) : -1;
+    real[h] = __ballot(src[h] >= 0);
   }
+  const int count = real[1] ? 128 - __clzll(real[1]) : real[0] ? 64 - __clzll(real[0]) : 0;
+  if (threadIdx.x < 64) {
+    const int first = real[0] ? __ffsll(real[0]) - 1 : real[1] ? 64 + __ffsll(real[1]) - 1 : 0;
+    const int any = first < 64 ? __shfl(src[0], first & 63) : __shfl(src[1], first & 63);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) rows[64 * h + lane] = src[h] >= 0 ? src[h] : any;  // a row that is read anyway
+  }
+  __syncthreads();
+  const int m = (count + 15) / 16;
+#define FF8_GO(M) many_rows<kSwiglu, M>(x, rows, tq, ts, blk.e, n0, N, K, active, blk, real, xs, out)
+  if (m == 1)
+    FF8_GO(1);
+  else if (m == 2)
+    FF8_GO(2);
+  else if (m == 3)
+    FF8_GO(3);
+  else if (m == 4)
+    FF8_GO(4);
+  else if (m == 5)
+    FF8_GO(5);
+  else if (m == 6)
+    FF8_GO(6);
+#undef FF8_GO
+  const int done = 16 * m;  // the padding rows behind
+  if (active)
+    for (int i = lane; i < (blk.n - done) * (kCols / 8); i += 64)
+      st16(out + (int64_t)(blk.row + done + i / (kCols / 8)) * n_out + n0 + i % (kCols / 8) * 8, u32x4{0u, 0u, 0u, 0u});
 }
 
 }  // namespace
@@ -233,13 +435,20 @@ hipError_t launch_pack_mxfp4(const uint8_t* q, const uint8_t* s, int64_t rows, i
 hipError_t launch_grouped_gemv_mxfp4(const uint16_t* x, int64_t x_rows, const uint8_t* tq, const uint8_t* ts,
                                      const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap,
                                      int64_t N, int64_t K, bool swiglu, uint16_t* out, hipStream_t st) {
-  // at most this many blocks of 16 rows; the workgroups walk those there are
-  const int64_t items = M_cap / 16 * (N / (kTiles * 16)), fill = 2 * (int64_t)device_cu_count();
-  const unsigned grid = (unsigned)(items < fill ? items : fill);
-  if (swiglu)
-    gemv_mxfp4_kernel<true><<<grid, kWaves * 64, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, out);
-  else
-    gemv_mxfp4_kernel<false><<<grid, kWaves * 64, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, out);
+  const int64_t n_out = swiglu ? N / 2 : N;
+  // rows an expert has, on average: T * top_k where the tokens are gathered, otherwise what 16-row padding leaves
+  const int64_t rows = top_k ? x_rows * top_k : M_cap - 15 * (int64_t)E;
+  if (rows >= 16 * (int64_t)E) {
+    const int64_t cols = kManyWaves * kTiles * (swiglu ? 8 : 16), nt = (n_out + cols - 1) / cols;
+    const int64_t blocks = M_cap / kManyRows + (E < M_cap / 16 ? E : M_cap / 16);
+    auto* const f = swiglu ? gemm_mxfp4_kernel<true> : gemm_mxfp4_kernel<false>;
+    f<<<(unsigned)(blocks * nt), kManyThreads, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, out);
+  } else {
+    constexpr int kWaves = 4;
+    auto* const f = swiglu ? gemv_mxfp4_kernel<true, kWaves> : gemv_mxfp4_kernel<false, kWaves>;
+    f<<<(unsigned)(M_cap / 16 * (N / (16 * kTiles))), kWaves * 64, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row,
+                                                                            top_k, N, K, out);
+  }
   return hipGetLastError();
 }
 
