@@ -88,25 +88,32 @@ __device__ __forceinline__ bf16x8_t decode8(uint32_t w, float scale) {
 
 // What a wave computes at a time: kTiles tiles of 16 weight rows (with kSwiglu half of them gate rows and half the
 // up rows beside them).  D = weights (16 x 32) times tokens^T (32 x 16): lane l holds token l % 16, weight rows
-// 4 (l / 16) .. + 3 of a tile.  The weights' tiles are read with column block s of their expert.
+// 4 (l / 16) .. + 3 of a tile.  The addresses are the same for all lanes but for the lane's own offset, so that they
+// stay in scalar registers.
 constexpr int kTiles = 4;
+struct Weights {
+  const uint8_t *q[kTiles], *s[kTiles];  // first column block of each tile's rows
+};
 template <bool kSwiglu>
-__device__ __forceinline__ void weight_tiles(int e, int64_t n0, int64_t N, int64_t kt, int64_t (&tile)[kTiles]) {
+__device__ __forceinline__ Weights weight_tiles(const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts, int e,
+                                                int64_t n0, int64_t N, int64_t kt) {
+  Weights w;
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     const int64_t n = kSwiglu ? (i < kTiles / 2 ? n0 + 16 * i : N / 2 + n0 + 16 * (i - kTiles / 2)) : n0 + 16 * i;
-    tile[i] = ((int64_t)e * N + n) / 16 * kt;
+    const int64_t tile = ((int64_t)e * N + n) / 16 * kt;
+    w.q[i] = tq + tile * 1024;
+    w.s[i] = ts + tile * 64;
   }
+  return w;
 }
-__device__ __forceinline__ void fetch_weights(const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts,
-                                              const int64_t (&tile)[kTiles], int64_t s, u32x4 (&w)[kTiles],
+__device__ __forceinline__ void fetch_weights(const Weights& p, int64_t block, u32x4 (&w)[kTiles],
                                               uint32_t (&sc)[kTiles]) {
-  const int lane = threadIdx.x & 63;
+  const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i) {
-    w[i] = ldnt16(tq + (tile[i] + s) * 1024 + lane * 16);
-    sc[i] = __builtin_nontemporal_load(ts + (tile[i] + s) * 64 + lane);
-  }
+  for (int i = 0; i < kTiles; ++i) w[i] = ldnt16(p.q[i] + block * 1024 + lane * 16);
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) sc[i] = __builtin_nontemporal_load(p.s[i] + block * 64 + lane);
 }
 // The wave's number, as a value that the compiler knows to be the same in all lanes: what depends on it alone is
 // computed once, in scalar registers.
@@ -123,10 +130,11 @@ __device__ __forceinline__ int source_of(int64_t row, const int32_t* __restrict_
   return src / top_k < x_rows ? src / top_k : -1;
 }
 
-// A lane's 16-byte piece p of row r of a 128-column block of x in LDS: pieces are exchanged within a row by the
-// row's number, so that 16 lanes that read one piece of 16 rows meet 16 different places (256-byte rows would put
-// them into the same banks).
-__device__ __forceinline__ int x_place(int r, int p) { return r * 16 + (p ^ (r & 15)); }
+// Where a 128-column block of x holds 16-byte piece p of row r in LDS.  Rows are 256 bytes, all 64 banks, so pieces
+// are exchanged within a row by a number of the row's own; with row + 4 (instead of the row, which measured one
+// conflict for every read) the 16 lanes that the hardware serves together -- 0-3, 12-15, 20-27 of a half wave, and
+// the others -- meet 16 different places, as rows of one piece (reads) and as pieces of two rows (writes).
+__device__ __forceinline__ int x_place(int r, int p) { return r * 16 + (p ^ ((r + 4) & 15)); }
 
 // ---- few rows per expert ----
 // A workgroup computes 64 weight rows for 16 token rows of one expert.  Its waves share the column blocks (wave w
@@ -165,8 +173,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
       xp[i] = reinterpret_cast<const u32x4*>(x + (int64_t)__shfl(src, mask >> q & 1 ? q : first) * K) + (lane & 15);
     }
     u32x4* const xs = reinterpret_cast<u32x4*>(&part[wave][0]);
-    int64_t tile[kTiles];
-    weight_tiles<kSwiglu>(e, n0, N, kt, tile);
+    const Weights w = weight_tiles<kSwiglu>(tq, ts, e, n0, N, kt);
     f32x4 acc[kTiles];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -174,7 +181,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
     uint32_t sb[2][kTiles];
     auto fetch = [&](int64_t s, int d) {
       keep_order();
-      fetch_weights(tq, ts, tile, s, wb[d], sb[d]);
+      fetch_weights(w, s, wb[d], sb[d]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) xb[d][i] = xp[i][s * 16];
       keep_order();
@@ -247,13 +254,30 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
 // buffers while it computes from the other.
 constexpr int kManyWaves = 4, kManyThreads = 64 * kManyWaves, kManyRows = 96;
 
-// Rows of block mb: its expert (-1 behind the last), first row and number of rows, a multiple of 16.  An expert's
-// rows are split evenly over the fewest blocks of at most 96.
+// Workgroup b of a launch runs on XCD b % 8.  Each XCD takes an eighth of the (row block, weight rows) items, in
+// order: the workgroups that read the same rows of x, and those that read the same weights for two row blocks of
+// one expert, then share an L2.
+//
+// An item's row block: its expert (-1 where there is none), first row, number of rows (a multiple of 16), and which
+// weight rows.  An expert's rows are split evenly over the fewest blocks of at most 96.
 struct RowBlock {
   int e, row, n;
+  unsigned col;
 };
-__device__ __forceinline__ RowBlock find_block(int mb, const int32_t* __restrict__ offsets, int E) {
+__device__ __forceinline__ RowBlock find_block(unsigned nt, const int32_t* __restrict__ offsets, int E) {
   const int lane = threadIdx.x & 63;
+  unsigned blocks = 0;
+  for (int e0 = 0; e0 < E; e0 += 64) {
+    const int i = e0 + lane;
+    unsigned nb = i < E ? (unsigned)(offsets[i + 1] - offsets[i] + kManyRows - 1) / kManyRows : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) nb += __shfl_xor(nb, d);
+    blocks += __builtin_amdgcn_readfirstlane(nb);
+  }
+  const unsigned per = (blocks * nt + 7) / 8, item = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (blockIdx.x / 8 >= per || item >= blocks * nt) return {-1, 0, 0, 0};
+  int mb = (int)(item / nt);
+  const unsigned col = item - mb * nt;
   for (int e0 = 0; e0 < E; e0 += 64) {
     const int i = e0 + lane;
     const int g0 = i < E ? offsets[i] : 0, g = i < E ? offsets[i + 1] - g0 : 0;
@@ -264,16 +288,17 @@ __device__ __forceinline__ RowBlock find_block(int mb, const int32_t* __restrict
       const int u = __shfl_up(end, d);
       if (lane >= d) end += u;
     }
-    const int total = __shfl(end, 63);
+    const int total = __builtin_amdgcn_readlane(end, 63);
     if (mb < total) {
       const int at = __ffsll(__ballot(end > mb)) - 1;
-      const int b = mb - __shfl(end - nb, at), n = __shfl(g, at), n_b = __shfl(nb, at);
-      const int per = ((n / 16 + n_b - 1) / n_b) * 16, left = n - b * per;
-      return {e0 + at, __shfl(g0, at) + b * per, left < per ? left : per};
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+      const int b = mb - of(end - nb), n = of(g), n_b = of(nb);
+      const int rows = ((n / 16 + n_b - 1) / n_b) * 16, left = n - b * rows;
+      return {e0 + at, of(g0) + b * rows, left < rows ? left : rows, col};
     }
     mb -= total;
   }
-  return {-1, 0, 0};
+  return {-1, 0, 0, 0};
 }
 
 // The products of one workgroup with kM x 16 token rows.
@@ -289,8 +314,7 @@ __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const 
   const u32x4* xp[kM];
 #pragma unroll
   for (int m = 0; m < kM; ++m) xp[m] = reinterpret_cast<const u32x4*>(x + (int64_t)rows[16 * m + t16] * K) + piece;
-  int64_t tile[kTiles];
-  weight_tiles<kSwiglu>(e, n0, N, kt, tile);
+  const Weights w = weight_tiles<kSwiglu>(tq, ts, e, n0, N, kt);
   f32x4 acc[kTiles][kM];
 #pragma unroll
   for (int i = 0; i < kTiles; ++i)
@@ -301,12 +325,19 @@ __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const 
 #pragma unroll
   for (int m = 0; m < kM; ++m) xb[m] = xp[m][0];
   keep_order();
-  fetch_weights(tq, ts, tile, 0, wb[0], sb[0]);
+  fetch_weights(w, 0, wb[0], sb[0]);
   keep_order();
-  fetch_weights(tq, ts, tile, kt > 1 ? 1 : 0, wb[1], sb[1]);
+  fetch_weights(w, kt > 1 ? 1 : 0, wb[1], sb[1]);
   keep_order();
 #pragma unroll
   for (int m = 0; m < kM; ++m) xs[x_place(16 * m + t16, piece)] = xb[m];
+  // the weights of 32 columns are decoded while the matrix instructions work on the 32 before
+  bf16x8_t a[2][kTiles];
+  auto decode = [&](int d, int j, bf16x8_t (&to)[kTiles]) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) to[i] = decode8(wb[d][i][j], __uint_as_float(sb[d][i] << 23));
+  };
+  decode(0, 0, a[0]);
   __syncthreads();
   for (int64_t s = 0; s < kt; s += 2) {
 #pragma unroll
@@ -318,24 +349,31 @@ __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const 
 #pragma unroll
       for (int m = 0; m < kM; ++m) xb[m] = xp[m][x_next * 16];
       keep_order();
-      {
-        const u32x4* const xd = xs + d * kManyRows * 16;
+      const u32x4* const xd = xs + d * kManyRows * 16;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          bf16x8_t a[kTiles];
-#pragma unroll
-          for (int i = 0; i < kTiles; ++i) a[i] = decode8(wb[d][i][j], __uint_as_float(sb[d][i] << 23));
-#pragma unroll
-          for (int m = 0; m < kM; ++m) {
-            const bf16x8_t b =
-                __builtin_bit_cast(bf16x8_t, xd[x_place(16 * m + (lane & 15), (lane >> 4) * 4 + j)]);
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-              acc[i][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b, acc[i][m], 0, 0, 0);
-          }
+      for (int j = 0; j < 4; ++j) {
+        if (j == 3) {
+          fetch_weights(w, w_next, wb[d], sb[d]);
+          keep_order();
         }
-        keep_order();
-        fetch_weights(tq, ts, tile, w_next, wb[d], sb[d]);
+        decode(j < 3 ? d : 1 - d, (j + 1) & 3, a[(j + 1) & 1]);
+#pragma unroll
+        for (int m = 0; m < kM; ++m) {
+          const bf16x8_t b = __builtin_bit_cast(bf16x8_t, xd[x_place(16 * m + (lane & 15), (lane >> 4) * 4 + j)]);
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i)
+            acc[i][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j & 1][i], b, acc[i][m], 0, 0, 0);
+        }
+        // issue order: two LDS reads ahead, then matrix instructions with decoding between them
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+        for (int m = 0; m < kM; ++m) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
         keep_order();
       }
 #pragma unroll
@@ -372,11 +410,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void gemm_mxfp4_kernel(
   __shared__ int rows[kManyRows];
   constexpr int kCols = kSwiglu ? kTiles * 8 : kTiles * 16;  // of out, a wave
   const int64_t n_out = kSwiglu ? N / 2 : N;
-  const unsigned nt = (unsigned)((n_out + kManyWaves * kCols - 1) / (kManyWaves * kCols)), mb = blockIdx.x / nt;
-  const RowBlock blk = find_block((int)mb, offsets, E);
+  const unsigned nt = (unsigned)((n_out + kManyWaves * kCols - 1) / (kManyWaves * kCols));
+  const RowBlock blk = find_block(nt, offsets, E);
   if (blk.e < 0 || blk.row + blk.n > M_cap) return;  // uniform
   const int lane = threadIdx.x & 63;
-  int64_t n0 = ((int64_t)(blockIdx.x - mb * nt) * kManyWaves + wave_number()) * kCols;
+  int64_t n0 = ((int64_t)blk.col * kManyWaves + wave_number()) * kCols;
   const bool active = n0 < n_out;  // not so for waves of the last workgroup where n_out is no multiple of its columns:
   if (!active) n0 = 0;             // they go along and store nothing
   unsigned long long real[2];
@@ -442,7 +480,7 @@ hipError_t launch_grouped_gemv_mxfp4(const uint16_t* x, int64_t x_rows, const ui
     const int64_t cols = kManyWaves * kTiles * (swiglu ? 8 : 16), nt = (n_out + cols - 1) / cols;
     const int64_t blocks = M_cap / kManyRows + (E < M_cap / 16 ? E : M_cap / 16);
     auto* const f = swiglu ? gemm_mxfp4_kernel<true> : gemm_mxfp4_kernel<false>;
-    f<<<(unsigned)(blocks * nt), kManyThreads, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, out);
+    f<<<(unsigned)((blocks * nt + 7) / 8 * 8), kManyThreads, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, out);
   } else {
     constexpr int kWaves = 4;
     auto* const f = swiglu ? gemv_mxfp4_kernel<true, kWaves> : gemv_mxfp4_kernel<false, kWaves>;
