@@ -443,7 +443,8 @@ int ff8_pack_mxfp4(const uint8_t* q, const ff8_e8m0* s, int64_t rows, int64_t co
  *   top_k    0: x [x_rows = M_cap, K] holds the grouped rows.  k >= 1: x [x_rows = T, K] holds the tokens, and row m
  *            takes token src_row[m] / top_k (src_row required): no permute is needed in front.
  *   out      [M_cap, N] bf16; rows >= offsets[E] untouched.
- *   E <= 1024; M_cap, N, K multiples of 128; x_rows and M_cap below 2^31; x, tq, ts and out 16-byte aligned.
+ *   E <= 1024; M_cap, N, K multiples of 128; x_rows and M_cap below 2^31, x_rows * K below 2^35, M_cap * N below
+ *   2^41; x, tq, ts and out 16-byte aligned.
  */
 int ff8_grouped_gemv_mxfp4(const ff8_bf16* x, int64_t x_rows, const uint8_t* tq, const ff8_e8m0* ts,
                            const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap, int64_t N,

@@ -474,6 +474,8 @@ static int gemv_mxfp4(const char* fn, const ff8_bf16* x, int64_t x_rows, const u
     return fail(FF8_ERR_SHAPE, "%s: M_cap, the weights' rows and K must be multiples of 128", fn);
   if (!(M_cap < ((int64_t)1 << 31) && x_rows >= 0 && x_rows < ((int64_t)1 << 31)))
     return fail(FF8_ERR_SHAPE, "%s: M_cap and x_rows must be below 2^31", fn);
+  if (!(x_rows < ((int64_t)1 << 35) / K && M_cap / 16 < ((int64_t)1 << 31) / (N / 64)))
+    return fail(FF8_ERR_SHAPE, "%s: x_rows * K must be below 2^35 and M_cap * N below 2^41", fn);
   if (top_k == 0 && x_rows != M_cap) return fail(FF8_ERR_SHAPE, "%s: grouped rows: x_rows must be M_cap", fn);
   if ((x_rows > 0 && !x) || !tq || !ts || !offsets || !out) return fail(FF8_ERR_NULL, "%s: a tensor is NULL", fn);
   if (top_k > 0 && !src_row) return fail(FF8_ERR_NULL, "%s: src_row is NULL", fn);

@@ -202,19 +202,30 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
-    // Two blocks in flight.  No load is behind a condition, so that the waits in front of a step count the loads
-    // behind it and leave them in flight; behind its last block a wave loads that one again.
+    // Two blocks in flight.  Inside a path no load is behind a condition, so that the waits in front of a step count
+    // the loads behind it and leave them in flight.
     const int64_t n = (kt - wave + kWaves - 1) / kWaves;
-    auto block = [&](int64_t i) { return wave + (i < n ? i : n - 1) * kWaves; };
-    if (n > 0) {
+    auto block = [&](int64_t i) { return wave + i * kWaves; };
+    if (n == 1) {
+      fetch(block(0), 0);
+      step(0);
+    } else if (n > 1) {
       fetch(block(0), 0);
       fetch(block(1), 1);
-      for (int64_t i = 0; i < n; i += 2) {
+      int64_t i = 0;
+      for (; i + 3 < n; i += 2) {
         step(0);
         fetch(block(i + 2), 0);
-        if (i + 1 == n) break;
         step(1);
         fetch(block(i + 3), 1);
+      }
+      step(0);
+      if (i + 2 < n) {
+        fetch(block(i + 2), 0);
+        step(1);
+        step(0);
+      } else {
+        step(1);
       }
     }
 #pragma unroll

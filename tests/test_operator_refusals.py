@@ -101,7 +101,8 @@ def test_mxfp4_products(lib, name):
     for bad in (dict(E=0), dict(E=1025), dict(top_k=-1), dict(x=ODD), dict(tq=ODD), dict(ts=ODD), dict(out=ODD)):
         assert call(**bad) == ARG, bad
     for bad in (dict(M=200), dict(M=0), dict(N=64), dict(N=192), dict(K=96), dict(K=0), dict(x_rows=100),
-                dict(top_k=2, x_rows=-1), dict(top_k=2, x_rows=1 << 31), dict(M=1 << 31, x_rows=1 << 31)):
+                dict(top_k=2, x_rows=-1), dict(top_k=2, x_rows=1 << 31), dict(M=1 << 31, x_rows=1 << 31),
+                dict(top_k=2, x_rows=1 << 28, K=1 << 7), dict(M=1 << 28, x_rows=1 << 28, N=1 << 13)):
         assert call(**bad) == SHAPE, bad
     for bad in (dict(x=None), dict(tq=None), dict(ts=None), dict(offsets=None), dict(out=None),
                 dict(src=None, top_k=1)):
