@@ -425,7 +425,8 @@ int ff8_quant_mxfp4(const ff8_bf16* w, int64_t rows, int64_t cols, uint8_t* q, f
  * ff8_pack_mxfp4 -- MXFP4 weights in the order in which the products read them, once per set of weights.
  *   q [rows, cols/2], s [rows, cols/32] as above (a stack of E expert weights [E, N, K] is rows = E*N).
  *   tq [rows/16, cols/128, 64, 16]: bytes 16 l .. 16 l + 15 of a tile are row l % 16, columns 32 (l / 16) ..
- *   + 31 of its 16 rows x 128 columns; ts [rows/16, cols/128, 64]: entry l is their scale.
+ *   + 31 of its 16 rows x 128 columns; ts [rows/32, cols/128, 64, 2]: bytes 2 l and 2 l + 1 are the scales of
+ *   lane l's groups in the two tiles of 32 rows.
  *   rows and cols multiples of 128, rows * cols < 2^37; q and tq 16-byte aligned and apart from one another.
  */
 int ff8_pack_mxfp4(const uint8_t* q, const ff8_e8m0* s, int64_t rows, int64_t cols, uint8_t* tq, ff8_e8m0* ts,

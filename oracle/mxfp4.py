@@ -52,17 +52,17 @@ def dequant(q, s):
 
 
 def pack(q, s):
-    """Tile order: tq [rows / 16, cols / 128, 64, 16], ts [rows / 16, cols / 128, 64]; lane l of a tile is
-    row l % 16, columns 32 * (l // 16) .. + 31."""
+    """Tile order: tq [rows / 16, cols / 128, 64, 16], ts [rows / 32, cols / 128, 64, 2]; lane l of a tile is
+    row l % 16, columns 32 * (l // 16) .. + 31, and its scales in two tiles stand side by side."""
     rows, half = q.shape
     kt = half // 64
     tq = np.zeros((rows // 16, kt, 64, 16), dtype=np.uint8)
-    ts = np.zeros((rows // 16, kt, 64), dtype=np.uint8)
+    ts = np.zeros((rows // 32, kt, 64, 2), dtype=np.uint8)
     for lane in range(64):
         r, g = lane % 16, lane // 16
         for c in range(kt):
             tq[:, c, lane] = q[r::16, c * 64 + g * 16: c * 64 + g * 16 + 16]
-            ts[:, c, lane] = s[r::16, c * 4 + g]
+            ts[:, c, lane] = s[r::16, c * 4 + g].reshape(-1, 2)
     return tq, ts
 
 

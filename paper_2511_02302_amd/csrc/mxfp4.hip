@@ -7,7 +7,7 @@
 // are float32.  With few rows the weights are the traffic, so they are stored in the order in which
 // the matrix instruction takes them (ff8_pack_mxfp4): a tile of 16 rows x 128 columns is 1 KiB in
 // which lane l's 16 bytes are row l % 16, columns 32 (l / 16) .. + 31 -- one scale group -- and a
-// wave's load is contiguous.  From row-major weights the same kernel reached 3.4 TB/s, from tiles 6.1
+// wave's load is contiguous; a lane's scales of the two tiles of 32 rows stand side by side.  From row-major weights the same kernel reached 3.4 TB/s, from tiles 6.1
 // (8 experts, 4096 x 7168, one row each): a wave's 16-byte loads then fall in 16 rows.
 
 #include <math.h>
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kThreads) void pack_mxfp4_kernel(const uint8_t* __r
   const int l = (int)(i & 63);
   const int64_t row = rb * 16 + (l & 15), piece = kt * 4 + (l >> 4);  // of k_tiles * 4 pieces in a row
   st16(tq + i * 16, ld16(q + (row * k_tiles * 4 + piece) * 16));
-  ts[i] = s[row * k_tiles * 4 + piece];
+  ts[(((rb >> 1) * k_tiles + kt) * 64 + l) * 2 + (rb & 1)] = s[row * k_tiles * 4 + piece];
 }
 
 __device__ __forceinline__ float swiglu(float g, float u) { return g / (1.0f + expf(-g)) * u; }
@@ -91,30 +91,36 @@ __device__ __forceinline__ bf16x8_t decode8(uint32_t w, float scale) {
 // 4 (l / 16) .. + 3 of a tile.  The addresses are the same for all lanes but for the lane's own offset, so that they
 // stay in scalar registers.
 constexpr int kTiles = 4;
-struct Weights {
-  const uint8_t *q[kTiles], *s[kTiles];  // first column block of each tile's rows
-};
 template <bool kSwiglu>
-__device__ __forceinline__ Weights weight_tiles(const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts, int e,
-                                                int64_t n0, int64_t N, int64_t kt) {
-  Weights w;
+struct Weights {
+  const uint8_t *q[kTiles], *s[kTiles / 2];  // at the first column block of the rows
+  struct Block {
+    u32x4 q[kTiles];
+    uint32_t s[kTiles / 2];
+    // tile i's scale in the lane's row and group, as a float
+    __device__ __forceinline__ float scale(int i) const {
+      return __uint_as_float(i & 1 ? s[i / 2] << 15 & 0x7F800000u : s[i / 2] << 23 & 0x7F800000u);
+    }
+  };
+  __device__ __forceinline__ Weights(const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts, int e, int64_t n0,
+                                     int64_t N, int64_t kt) {
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i) {
-    const int64_t n = kSwiglu ? (i < kTiles / 2 ? n0 + 16 * i : N / 2 + n0 + 16 * (i - kTiles / 2)) : n0 + 16 * i;
-    const int64_t tile = ((int64_t)e * N + n) / 16 * kt;
-    w.q[i] = tq + tile * 1024;
-    w.s[i] = ts + tile * 64;
+    for (int i = 0; i < kTiles; ++i) {
+      const int64_t n = kSwiglu ? (i < kTiles / 2 ? n0 + 16 * i : N / 2 + n0 + 16 * (i - kTiles / 2)) : n0 + 16 * i;
+      const int64_t tile = ((int64_t)e * N + n) / 16;
+      q[i] = tq + tile * kt * 1024;
+      if (i % 2 == 0) s[i / 2] = ts + tile * kt * 64;
+    }
   }
-  return w;
-}
-__device__ __forceinline__ void fetch_weights(const Weights& p, int64_t block, u32x4 (&w)[kTiles],
-                                              uint32_t (&sc)[kTiles]) {
-  const uint32_t lane = threadIdx.x & 63;
+  __device__ __forceinline__ void fetch(int64_t block, Block& b) const {
+    const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i) w[i] = ldnt16(p.q[i] + block * 1024 + lane * 16);
+    for (int i = 0; i < kTiles; ++i) b.q[i] = ldnt16(q[i] + block * 1024 + lane * 16);
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i) sc[i] = __builtin_nontemporal_load(p.s[i] + block * 64 + lane);
-}
+    for (int i = 0; i < kTiles / 2; ++i)
+      b.s[i] = __builtin_nontemporal_load(reinterpret_cast<const uint16_t*>(s[i] + block * 128 + lane * 2));
+  }
+};
 // The wave's number, as a value that the compiler knows to be the same in all lanes: what depends on it alone is
 // computed once, in scalar registers.
 __device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
@@ -142,6 +148,81 @@ __device__ __forceinline__ int x_place(int r, int p) { return r * 16 + (p ^ ((r 
 // LDS and are added in wave order.  Groups are multiples of 16 rows, so block b is rows 16 b .. + 15 and only its
 // expert has to be looked up.  A wave brings its own piece of x through LDS into the order of the matrix
 // instruction; in registers it has two blocks of weights and x in flight.
+//
+// The products of a wave's blocks, into its part of LDS.  kX: 16-byte pieces of x that a lane brings for a block,
+// four rows each; with one only the first four rows are there (the other columns of the products are not stored).
+template <bool kSwiglu, int kWaves, int kX>
+__device__ __forceinline__ void few_rows(const uint16_t* __restrict__ x, int src, unsigned mask,
+                                         const Weights<kSwiglu>& w, int wave, int64_t K, float* part) {
+  const int lane = threadIdx.x & 63;
+  const int64_t kt = K / kTile;
+  // row 4 i + lane / 16, piece lane % 16 of a block; padding rows read one that is read anyway
+  const int first = __ffs(mask) - 1;
+  const u32x4* xp[kX];
+#pragma unroll
+  for (int i = 0; i < kX; ++i) {
+    const int q = 4 * i + (lane >> 4);
+    xp[i] = reinterpret_cast<const u32x4*>(x + (int64_t)__shfl(src, mask >> q & 1 ? q : first) * K) + (lane & 15);
+  }
+  u32x4* const xs = reinterpret_cast<u32x4*>(part);
+  f32x4 acc[kTiles];
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  typename Weights<kSwiglu>::Block wb[2];
+  u32x4 xb[2][kX];
+  auto fetch = [&](int64_t i, int d) {
+    const int64_t s = wave + i * kWaves;
+    keep_order();
+    w.fetch(s, wb[d]);
+#pragma unroll
+    for (int r = 0; r < kX; ++r) xb[d][r] = xp[r][s * 16];
+    keep_order();
+  };
+  auto step = [&](int d) {
+#pragma unroll
+    for (int i = 0; i < kX; ++i) xs[x_place(4 * i + (lane >> 4), lane & 15)] = xb[d][i];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bf16x8_t b = __builtin_bit_cast(bf16x8_t, xs[x_place(lane & 15, (lane >> 4) * 4 + j)]);
+      bf16x8_t a[kTiles];
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) a[i] = decode8(wb[d].q[i][j], wb[d].scale(i));
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b, acc[i], 0, 0, 0);
+      keep_order();  // decoding all of the block first would take 64 more registers
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  // Two blocks in flight.  Inside a path no load is behind a condition, so that the waits in front of a step count
+  // the loads behind it and leave them in flight.
+  const int64_t n = (kt - wave + kWaves - 1) / kWaves;
+  if (n == 1) {
+    fetch(0, 0);
+    step(0);
+  } else if (n > 1) {
+    fetch(0, 0);
+    fetch(1, 1);
+    int64_t i = 0;
+    for (; i + 3 < n; i += 2) {
+      step(0);
+      fetch(i + 2, 0);
+      step(1);
+      fetch(i + 3, 1);
+    }
+    step(0);
+    if (i + 2 < n) {
+      fetch(i + 2, 0);
+      step(1);
+      step(0);
+    } else {
+      step(1);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) *reinterpret_cast<f32x4*>(&part[i * 256 + lane * 4]) = acc[i];
+}
+
 template <bool kSwiglu, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
     const uint16_t* __restrict__ x, int64_t x_rows, const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts,
@@ -150,7 +231,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
   __shared__ float part[kWaves][kTiles * 256];  // also x, a block a wave
   const int lane = threadIdx.x & 63, wave = wave_number();
   constexpr int kCols = kSwiglu ? kTiles * 8 : kTiles * 16;  // columns of out that a workgroup writes
-  const int64_t n_out = kSwiglu ? N / 2 : N, kt = K / kTile;
+  const int64_t n_out = kSwiglu ? N / 2 : N;
   const unsigned nt = (unsigned)(n_out / kCols), mb = blockIdx.x / nt;
   const int64_t n0 = (int64_t)(blockIdx.x - mb * nt) * kCols, row0 = (int64_t)mb * 16;
   const int src = source_of(row0 + (lane & 15), src_row, top_k, x_rows);  // rows below M_cap; used below offsets[E]
@@ -163,74 +244,11 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
   }
   if (e < 0) return;  // behind the last group; the same for the whole workgroup
   const unsigned mask = (unsigned)__ballot(src >= 0) & 0xFFFFu;
-  if (mask) {
-    // the rows a lane brings: row 4 i + lane / 16, piece lane % 16 of a block; padding rows read one that is read anyway
-    const int first = __ffs(mask) - 1;
-    const u32x4* xp[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int q = 4 * i + (lane >> 4);
-      xp[i] = reinterpret_cast<const u32x4*>(x + (int64_t)__shfl(src, mask >> q & 1 ? q : first) * K) + (lane & 15);
-    }
-    u32x4* const xs = reinterpret_cast<u32x4*>(&part[wave][0]);
-    const Weights w = weight_tiles<kSwiglu>(tq, ts, e, n0, N, kt);
-    f32x4 acc[kTiles];
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    u32x4 wb[2][kTiles], xb[2][4];
-    uint32_t sb[2][kTiles];
-    auto fetch = [&](int64_t s, int d) {
-      keep_order();
-      fetch_weights(w, s, wb[d], sb[d]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xb[d][i] = xp[i][s * 16];
-      keep_order();
-    };
-    auto step = [&](int d) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xs[x_place(4 * i + (lane >> 4), lane & 15)] = xb[d][i];
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bf16x8_t b = __builtin_bit_cast(bf16x8_t, xs[x_place(lane & 15, (lane >> 4) * 4 + j)]);
-        bf16x8_t a[kTiles];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) a[i] = decode8(wb[d][i][j], __uint_as_float(sb[d][i] << 23));
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b, acc[i], 0, 0, 0);
-        keep_order();  // decoding all of the block first would take 64 more registers
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    };
-    // Two blocks in flight.  Inside a path no load is behind a condition, so that the waits in front of a step count
-    // the loads behind it and leave them in flight.
-    const int64_t n = (kt - wave + kWaves - 1) / kWaves;
-    auto block = [&](int64_t i) { return wave + i * kWaves; };
-    if (n == 1) {
-      fetch(block(0), 0);
-      step(0);
-    } else if (n > 1) {
-      fetch(block(0), 0);
-      fetch(block(1), 1);
-      int64_t i = 0;
-      for (; i + 3 < n; i += 2) {
-        step(0);
-        fetch(block(i + 2), 0);
-        step(1);
-        fetch(block(i + 3), 1);
-      }
-      step(0);
-      if (i + 2 < n) {
-        fetch(block(i + 2), 0);
-        step(1);
-        step(0);
-      } else {
-        step(1);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) *reinterpret_cast<f32x4*>(&part[wave][i * 256 + lane * 4]) = acc[i];
-  }
+  const Weights<kSwiglu> w(tq, ts, e, n0, N, K / kTile);
+  if (mask & 0xFFF0u)
+    few_rows<kSwiglu, kWaves, 4>(x, src, mask, w, wave, K, part[wave]);
+  else if (mask)
+    few_rows<kSwiglu, kWaves, 1>(x, src, mask, w, wave, K, part[wave]);
   __syncthreads();
   // elements q, q + 1: tile q / 256, token (q / 4) % 16, weight rows 4 ((q / 64) % 4) + q % 4 .. + 1 of the tile
   for (int q = 2 * threadIdx.x; q < kCols * 16; q += kWaves * 128) {
@@ -238,16 +256,16 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
     f32x2 v = {0.0f, 0.0f};
     if (mask >> token & 1) {
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const f32x2 p = *reinterpret_cast<const f32x2*>(&part[w][q]);
+      for (int i = 0; i < kWaves; ++i) {
+        const f32x2 p = *reinterpret_cast<const f32x2*>(&part[i][q]);
         v[0] += p[0];
         v[1] += p[1];
       }
       if (kSwiglu) {
         f32x2 u = {0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const f32x2 p = *reinterpret_cast<const f32x2*>(&part[w][q + kTiles * 128]);
+        for (int i = 0; i < kWaves; ++i) {
+          const f32x2 p = *reinterpret_cast<const f32x2*>(&part[i][q + kTiles * 128]);
           u[0] += p[0];
           u[1] += p[1];
         }
@@ -325,20 +343,20 @@ __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const 
   const u32x4* xp[kM];
 #pragma unroll
   for (int m = 0; m < kM; ++m) xp[m] = reinterpret_cast<const u32x4*>(x + (int64_t)rows[16 * m + t16] * K) + piece;
-  const Weights w = weight_tiles<kSwiglu>(tq, ts, e, n0, N, kt);
+  const Weights<kSwiglu> w(tq, ts, e, n0, N, kt);
   f32x4 acc[kTiles][kM];
 #pragma unroll
   for (int i = 0; i < kTiles; ++i)
 #pragma unroll
     for (int m = 0; m < kM; ++m) acc[i][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  u32x4 wb[2][kTiles], xb[kM];
-  uint32_t sb[2][kTiles];
+  typename Weights<kSwiglu>::Block wb[2];
+  u32x4 xb[kM];
 #pragma unroll
   for (int m = 0; m < kM; ++m) xb[m] = xp[m][0];
   keep_order();
-  fetch_weights(w, 0, wb[0], sb[0]);
+  w.fetch(0, wb[0]);
   keep_order();
-  fetch_weights(w, kt > 1 ? 1 : 0, wb[1], sb[1]);
+  w.fetch(kt > 1 ? 1 : 0, wb[1]);
   keep_order();
 #pragma unroll
   for (int m = 0; m < kM; ++m) xs[x_place(16 * m + t16, piece)] = xb[m];
@@ -346,7 +364,7 @@ __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const 
   bf16x8_t a[2][kTiles];
   auto decode = [&](int d, int j, bf16x8_t (&to)[kTiles]) {
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) to[i] = decode8(wb[d][i][j], __uint_as_float(sb[d][i] << 23));
+    for (int i = 0; i < kTiles; ++i) to[i] = decode8(wb[d].q[i][j], wb[d].scale(i));  // (the hardware reads a scale's exponent alone)
   };
   decode(0, 0, a[0]);
   __syncthreads();
@@ -364,7 +382,7 @@ __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (j == 3) {
-          fetch_weights(w, w_next, wb[d], sb[d]);
+          w.fetch(w_next, wb[d]);
           keep_order();
         }
         decode(j < 3 ? d : 1 - d, (j + 1) & 3, a[(j + 1) & 1]);

@@ -551,11 +551,12 @@ def ff8_quant_mxfp4(w, q, s, stream=None):
 
 
 def ff8_pack_mxfp4(q, s, tq, ts, stream=None):
-    """q [E, N, K // 2], s [E, N, K // 32] -> tq [E, N // 16, K // 128, 64, 16], ts [E, N // 16, K // 128, 64]."""
+    """q [E, N, K // 2], s [E, N, K // 32] -> tq [E, N // 16, K // 128, 64, 16], ts of E * N * K // 32 bytes
+    (ordered [E, N // 32, K // 128, 64, 2], any shape)."""
     E, N, half = q.shape
     K = 2 * half
     _shape(s, (E, N, K // 32), "s"); _shape(tq, (E, N // 16, K // 128, 64, 16), "tq")
-    _shape(ts, (E, N // 16, K // 128, 64), "ts")
+    _numel(ts, E * N * K // 32, "ts")
     args = [_ptr(q, _u8, "q", 3), _ptr(s, _u8, "s", 3), E * N, K, _ptr(tq, _u8, "tq"), _ptr(ts, _u8, "ts")]
     _here(stream, q, s, tq, ts)
     _check(load().ff8_pack_mxfp4(*args, _stream(stream)), "ff8_pack_mxfp4")
@@ -566,7 +567,7 @@ def _gemv_mxfp4(name, cols, x, tq, ts, offsets, out, src_row, top_k, stream):
     E, nt, _, _, _ = tq.shape
     N = 16 * nt
     M_cap = out.shape[0]
-    _shape(tq, (E, nt, K // 128, 64, 16), "tq"); _shape(ts, (E, nt, K // 128, 64), "ts")
+    _shape(tq, (E, nt, K // 128, 64, 16), "tq"); _numel(ts, E * N * K // 32, "ts")
     _numel(offsets, E + 1, "offsets"); _numel(src_row, M_cap, "src_row"); _shape(out, (M_cap, N // cols), "out")
     if N % cols:
         raise ValueError("tq must have shape (E, 2I // 16, K // 128, 64, 16)")

@@ -257,7 +257,7 @@ class ExpertLayerFP4:
         self.score, self.normalize, self.scale = score, normalize, scale
         self.device = dev = torch.device(device)
         M = self.rows(T)
-        tiles = lambda n, k_: (((E, n // 16, k_ // 128, 64, 16), _u8), ((E, n // 16, k_ // 128, 64), _u8))  # noqa: E731
+        tiles = lambda n, k_: (((E, n // 16, k_ // 128, 64, 16), _u8), ((E, n // 32, k_ // 128, 64, 2), _u8))  # noqa: E731
         spec = {"ws": ((max(1, ff8.ff8_permute_workspace_bytes(T, k, E)),), _u8),
                 "topk_idx": ((T, k), _i32), "probs": ((T, k), _f32), "row_map": ((T, k), _i32),
                 "offsets": ((E + 1,), _i32), "src_row": ((M,), _i32),

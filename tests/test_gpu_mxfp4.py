@@ -39,7 +39,7 @@ def test_pack(E, N, K):
     g = torch.Generator().manual_seed(N)
     q = torch.randint(0, 256, (E, N, K // 2), generator=g, dtype=torch.uint8)
     s = torch.randint(0, 256, (E, N, K // 32), generator=g, dtype=torch.uint8)
-    tq, ts = poisoned((E, N // 16, K // 128, 64, 16), torch.uint8), poisoned((E, N // 16, K // 128, 64), torch.uint8)
+    tq, ts = poisoned((E, N // 16, K // 128, 64, 16), torch.uint8), poisoned((E, N // 32, K // 128, 64, 2), torch.uint8)
     ff8.ff8_pack_mxfp4(q.cuda(), s.cuda(), tq, ts)
     torch.cuda.synchronize()
     for e in range(E):
@@ -53,7 +53,7 @@ def _weights(E, N, K, seed, lo=119, hi=122):
     q = torch.randint(0, 256, (E, N, K // 2), generator=g, dtype=torch.uint8)
     s = torch.randint(lo, hi, (E, N, K // 32), generator=g, dtype=torch.uint8)
     tq = torch.empty((E, N // 16, K // 128, 64, 16), dtype=torch.uint8, device="cuda")
-    ts = torch.empty((E, N // 16, K // 128, 64), dtype=torch.uint8, device="cuda")
+    ts = torch.empty((E, N // 32, K // 128, 64, 2), dtype=torch.uint8, device="cuda")
     ff8.ff8_pack_mxfp4(q.cuda(), s.cuda(), tq, ts)
     return [mxfp4.dequant(q[e].numpy(), s[e].numpy()) for e in range(E)], tq, ts
 
@@ -166,7 +166,7 @@ def test_extreme_scales_and_values():
                            (127, 7, 2.0 ** -133)):
         q = torch.full((1, N, K // 2), code * 17, dtype=torch.uint8)
         s = torch.full((1, N, K // 32), byte, dtype=torch.uint8)
-        tq, ts = torch.empty((1, N // 16, 1, 64, 16), dtype=torch.uint8, device="cuda"), torch.empty((1, N // 16, 1, 64), dtype=torch.uint8, device="cuda")
+        tq, ts = torch.empty((1, N // 16, 1, 64, 16), dtype=torch.uint8, device="cuda"), torch.empty((1, N // 32, 1, 64, 2), dtype=torch.uint8, device="cuda")
         ff8.ff8_pack_mxfp4(q.cuda(), s.cuda(), tq, ts)
         offsets, src, M_cap = _groups([3], 16)
         x = torch.full((M_cap, K), xv, dtype=torch.bfloat16)
@@ -183,7 +183,7 @@ def test_scale_of_nan_reaches_its_rows_alone():
     q = torch.randint(0, 256, (E, N, K // 2), generator=g, dtype=torch.uint8)
     s = torch.full((E, N, K // 32), 120, dtype=torch.uint8)
     s[0, 37, 3] = 255
-    tq, ts = torch.empty((E, N // 16, K // 128, 64, 16), dtype=torch.uint8, device="cuda"), torch.empty((E, N // 16, K // 128, 64), dtype=torch.uint8, device="cuda")
+    tq, ts = torch.empty((E, N // 16, K // 128, 64, 16), dtype=torch.uint8, device="cuda"), torch.empty((E, N // 32, K // 128, 64, 2), dtype=torch.uint8, device="cuda")
     ff8.ff8_pack_mxfp4(q.cuda(), s.cuda(), tq, ts)
     offsets, src, M_cap = _groups([20], 16)
     out = poisoned((M_cap, N), torch.bfloat16)
@@ -231,7 +231,7 @@ def test_weights_past_four_gigabytes():
     """Tile offsets past 32 bits: 18 experts of 4096 x 131072 codes (4.8 GB); the last expert's rows."""
     E, N, K = 18, 4096, 131072
     tq = torch.zeros((E, N // 16, K // 128, 64, 16), dtype=torch.uint8, device="cuda")
-    ts = torch.full((E, N // 16, K // 128, 64), 127, dtype=torch.uint8, device="cuda")
+    ts = torch.full((E, N // 32, K // 128, 64, 2), 127, dtype=torch.uint8, device="cuda")
     tq[E - 1, :, -1] = 0x22  # ones in the last 128 columns
     offsets = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
     offsets[E] = 16

@@ -115,7 +115,7 @@ def test_binding_checks_shapes_and_types():
     e = lambda *shape, dtype=bf16: torch.empty(shape, dtype=dtype)  # noqa: E731
     T, E, k, H, M, N, K = 16, 8, 2, 256, 256, 384, 256
     idx, w, off, src = e(T, k, dtype=i32), e(T, k, dtype=f32), e(E + 1, dtype=i32), e(M, dtype=i32)
-    tq, ts = e(E, N // 16, K // 128, 64, 16, dtype=u8), e(E, N // 16, K // 128, 64, dtype=u8)
+    tq, ts = e(E, N // 16, K // 128, 64, 16, dtype=u8), e(E, N // 32, K // 128, 64, 2, dtype=u8)
     wrong = [
         lambda: ff8.ff8_router_topk(e(T, E), e(T - 1, k, dtype=i32), w),
         lambda: ff8.ff8_router_topk(e(T, E), idx, e(T, k + 1, dtype=f32)),

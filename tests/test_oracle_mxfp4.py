@@ -28,12 +28,12 @@ def test_scale_rule():
 
 def test_quant_error_and_pack():
     rng = np.random.default_rng(0)
-    w = rng.normal(size=(32, 256)) * 0.02
+    w = rng.normal(size=(64, 256)) * 0.02
     q, s = mxfp4.quant(w)
     # half of the widest step (2 * 2^T, between 4 and 6) with 3 * 2^T < amax
     step = np.repeat(np.exp2(s.astype(np.float64) - 127), 32, axis=1)
     assert np.all(np.abs(mxfp4.dequant(q, s) - w) <= step)
     tq, ts = mxfp4.pack(q, s)
-    assert tq.shape == (2, 2, 64, 16) and ts.shape == (2, 2, 64)
-    assert np.array_equal(tq[1, 1, 35], q[16 + 3, 64 + 32: 64 + 48]) and ts[1, 1, 35] == s[19, 4 + 2]
+    assert tq.shape == (4, 2, 64, 16) and ts.shape == (2, 2, 64, 2)
+    assert np.array_equal(tq[1, 1, 35], q[16 + 3, 64 + 32: 64 + 48]) and ts[0, 1, 35, 1] == s[19, 4 + 2]
     assert np.array_equal(np.sort(tq.reshape(-1)), np.sort(q.reshape(-1)))
