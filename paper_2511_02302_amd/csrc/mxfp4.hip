@@ -503,10 +503,15 @@ hipError_t launch_grouped_gemv_mxfp4(const uint16_t* x, int64_t x_rows, const ui
                                      const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap,
                                      int64_t N, int64_t K, bool swiglu, uint16_t* out, hipStream_t st) {
   const int64_t n_out = swiglu ? N / 2 : N;
-  // rows an expert has, on average: T * top_k where the tokens are gathered, otherwise what 16-row padding leaves
+  const int64_t cols = kManyWaves * kTiles * (swiglu ? 8 : 16), nt = (n_out + cols - 1) / cols;
+  // rows of all experts: T * top_k where the tokens are gathered, otherwise what 16-row padding leaves
   const int64_t rows = top_k ? x_rows * top_k : M_cap - 15 * (int64_t)E;
-  if (rows >= 16 * (int64_t)E) {
-    const int64_t cols = kManyWaves * kTiles * (swiglu ? 8 : 16), nt = (n_out + cols - 1) / cols;
+  // Blocks of 96 rows instead of 16 (times in us, 16 / 96):
+  //  * from 12 rows an expert on.  7168 wide, 32 experts, up projection: 8 rows 81 / 83, 12 92 / 84, 24 158 / 89;
+  //    2048 wide, 64 experts, down: 4 rows 24 / 23, 12 26 / 22; with skewed routing 8 rows 25 / 30, 12 33 / 28.
+  //  * and from 5/8 of an item per CU on: a workgroup of the 96-row form goes through all of K by itself.  4096 wide, 8
+  //    experts: 72 items 13 / 30, 144 7.6 / 11.5 and 44 / 46, 208 19 / 17, 232 80 / 54; 1024 wide: 116 18 / 19, 200 31 / 21.
+  if (rows >= 12 * (int64_t)E && (E + rows / kManyRows) * nt >= (int64_t)device_cu_count() * 5 / 8) {
     const int64_t blocks = M_cap / kManyRows + (E < M_cap / 16 ? E : M_cap / 16);
     auto* const f = swiglu ? gemm_mxfp4_kernel<true> : gemm_mxfp4_kernel<false>;
     f<<<(unsigned)((blocks * nt + 7) / 8 * 8), kManyThreads, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, out);

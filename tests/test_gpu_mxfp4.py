@@ -146,6 +146,43 @@ def test_swiglu_of_gathered_tokens(counts, align, I, K, T, k):
     _swiglu_check(out, xs, w, offsets, src, I)
 
 
+# experts with many rows beside some with few and none: enough of them for the form with 96-row blocks
+MANY = [0, 1, 5, 16, 17, 40, 64, 79, 80, 96, 97, 130, 200, 33, 0, 12]
+
+
+@pytest.mark.parametrize("N,K,align,copies", [(640, 128, 16, 8), (1408, 384, 16, 4), (256, 1408, 128, 14), (2048, 640, 32, 3)])
+def test_many_rows_product(N, K, align, copies):
+    counts = MANY * copies
+    E = len(counts)
+    w, tq, ts = _weights(E, N, K, N + K)
+    offsets, src, M_cap = _groups(counts, align, seed=1, extra=300)
+    x = _bf16((M_cap, K), 1)
+    x[torch.from_numpy((src < 0) | (np.arange(M_cap) >= offsets[-1]))] = float("nan")  # not read
+    out = poisoned((M_cap, N), torch.bfloat16)
+    ff8.ff8_grouped_gemv_mxfp4(x.cuda(), tq, ts, torch.from_numpy(offsets).cuda(), out,
+                               src_row=torch.from_numpy(src).cuda())
+    torch.cuda.synchronize()
+    xs = np.nan_to_num(f64(x))
+    _check_rows(out, moe_product(xs, w, offsets), _bound(xs, w, offsets), offsets, src)
+
+
+@pytest.mark.parametrize("I,K,T,k,align,copies", [(384, 256, 250, 3, 16, 4), (128, 896, 400, 2, 16, 12), (1408, 128, 201, 1, 64, 2)])
+def test_many_rows_swiglu_of_gathered_tokens(I, K, T, k, align, copies):
+    counts = MANY * copies
+    E = len(counts)
+    w, tq, ts = _weights(E, 2 * I, K, I + K)
+    offsets, src, M_cap = _groups(counts, align, T, k, seed=2, extra=200)
+    T_all = max(T, 12 * E // k + 1)  # more tokens in x than any row takes: what counts for the form is their number
+    x = _bf16((T_all, K), 3)
+    out = poisoned((M_cap, I), torch.bfloat16)
+    ff8.ff8_grouped_gemv_mxfp4_swiglu(x.cuda(), tq, ts, torch.from_numpy(offsets).cuda(), out,
+                                      src_row=torch.from_numpy(src).cuda(), top_k=k)
+    torch.cuda.synchronize()
+    m = int(offsets[-1])
+    xs = np.where(src[:m, None] >= 0, f64(x)[np.maximum(src[:m], 0) // k], 0.0)
+    _swiglu_check(out, xs, w, offsets, src, I)
+
+
 def test_source_rows_out_of_range_give_zeros():
     w, tq, ts = _weights(1, 128, 256, 0)
     offsets, src, M_cap = _groups([16], 16)
