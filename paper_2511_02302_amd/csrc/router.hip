@@ -202,15 +202,90 @@ __device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], 
   }
 }
 
+// The same by ranks, for 16 lanes and k <= 8, where that takes a fraction of the rounds' instructions: the k-th of
+// the lanes' largest keys bounds the k-th of all from below; the keys from there on (11 of 256 on average) go to
+// the lanes in expert order, one each (two each where a group of the wave has more than 16), and each lane counts
+// the better ones.  False, with nothing chosen, where there are more than 32.  Leaves the keys as they are.
+template <int N>
+__device__ __forceinline__ float from_left(float v) {  // of the lane N to the left, around the row
+  return __uint_as_float(dpp<0x120 + N>(__float_as_uint(v)));
+}
+template <int N>
+__device__ __forceinline__ int count_larger(float v, int n) {
+  if constexpr (N < 16) return count_larger<N + 1>(v, n + (from_left<N>(v) > v));
+  return n;
+}
+// Of the row's values `o`, how many come before this lane's v: larger, or equal and in a lane below `lane`
+// (kSelf: the lane's own `o` is another value, and counts as one in a lane below).
+template <int N, bool kSelf>
+__device__ __forceinline__ int count_before(float o, float v, int lane, int n) {
+  if constexpr (N < 16) {
+    const float f = N == 0 ? o : from_left<N == 0 ? 1 : N>(o);
+    if (N > 0 || kSelf) n += (f > v) | ((f == v) & (lane >= N));
+    return count_before<N + 1, kSelf>(o, v, lane, n);
+  }
+  return n;
+}
+__device__ __forceinline__ int row_inclusive_sum(int v) {
+  v += (int)dpp<0x111>((uint32_t)v);
+  v += (int)dpp<0x112>((uint32_t)v);
+  v += (int)dpp<0x114>((uint32_t)v);
+  v += (int)dpp<0x118>((uint32_t)v);
+  return v;
+}
+template <int V>
+__device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float (&l)[V], int k, Choice* out) {
+  const int lane = threadIdx.x & 15;
+  float best = key[0];
+#pragma unroll
+  for (int v = 1; v < V; ++v) best = fmaxf(best, key[v]);
+  const float bound = -group_max<16>(count_larger<1>(best, 0) < k ? -best : -INFINITY);
+  int n = 0;
+#pragma unroll
+  for (int v = 0; v < V; ++v) n += (key[v] >= bound) & (key[v] > -INFINITY);
+  const int end = row_inclusive_sum(n), total = (int)dpp<0x15F>((uint32_t)end);
+  if (__any(total > 32)) return false;
+  int at = end - n;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if ((key[v] >= bound) & (key[v] > -INFINITY)) out[at++] = {lane * V + v, l[v], key[v]};
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  Choice c = {-1, -INFINITY, -INFINITY}, d = c;
+  if (lane < total) c = out[lane];
+  int rank = count_before<0, false>(c.key, c.key, lane, 0);
+  if (__any(total > 16)) {
+    if (lane + 16 < total) d = out[lane + 16];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // every value of the first sixteen stands before an equal one of the second
+    rank += count_before<0, true>(d.key, c.key, -1, 0);
+    const int rank_d = count_before<0, false>(d.key, d.key, lane, 0) + count_before<0, true>(c.key, d.key, 16, 0);
+    if (rank_d < k) out[rank_d] = d;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (rank < k) out[rank] = c;
+  return true;
+}
+
+// True if the chosen keys are still there (the rounds leave -inf in their place).
+template <int L, int V>
+__device__ __forceinline__ bool choose(float (&key)[V], const float (&l)[V], int k, Choice* out) {
+  if constexpr (L == 16 && V > 1) {
+    if (k <= 8 && choose_ranked<V>(key, l, k, out)) return true;
+  }
+  choose_rounds<L, V>(key, l, k, out);
+  return false;
+}
+
 template <int L, int V, bool kSigmoid, bool kNormalize, bool kBias, typename X>
 __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ logits, const float* __restrict__ bias,
                                                         int64_t T, int E, int k, float scale, bool vec,
                                                         bool vec_bias, int32_t* __restrict__ topk_idx, float* __restrict__ probs) {
   constexpr bool kPacked = sizeof(X) == 2 && !kBias;
   constexpr bool kFull = !kSigmoid && (kBias || !kNormalize);  // the softmax over all experts is needed
-  __shared__ Choice found[kPacked ? 1 : kThreads];             // k <= L slots a group
+  constexpr int kFound = L == 16 ? 32 : 64;  // slots a group: k, or the candidates for them
+  __shared__ Choice found[kPacked ? 1 : kThreads / L * kFound];
   const int lane = threadIdx.x & (L - 1);
-  Choice* const mine = &found[kPacked ? 0 : threadIdx.x & ~(L - 1)];
+  Choice* const mine = &found[kPacked ? 0 : threadIdx.x / L * kFound];
   const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
   if (t >= T) return;  // whole groups of L lanes
   X raw[V], missing;
@@ -253,7 +328,7 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
     if (!kBias) {
 #pragma unroll
       for (int v = 0; v < V; ++v) key[v] = l[v] > -INFINITY ? l[v] : -INFINITY;  // NaN is never chosen
-      choose_rounds<L, V>(key, l, k, mine);
+      choose<L, V>(key, l, k, mine);
     } else {
       // In float32 first.  Both scores are off by less than 2^-21 (sigmoid: the exponential's and the
       // reciprocal's unit, damped) or 2^-18 of the row's largest (softmax: a sum of up to 1024), the sum by
@@ -268,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
         const float sum_b = s + b[v];
         key[v] = ((l[v] > -INFINITY) & (sum_b > -INFINITY)) ? sum_b : -INFINITY;
       }
-      choose_rounds<L, V>(key, l, k, mine);
+      const bool kept = choose<L, V>(key, l, k, mine);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       const float err = kSigmoid ? 0x1p-19f : 0x1p-16f * inv;
       bool unsure = false;
@@ -278,11 +353,18 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
           unsure = !(a.logit == n.logit && bias[a.idx] == bias[n.idx]);
       }
       const Choice last = mine[k - 1];
-      if (last.idx >= 0) {
-        const float lb = bias[last.idx], near = last.key - (err + 0x1p-21f * fabsf(last.key));
+      const float near = last.key - (err + 0x1p-21f * fabsf(last.key));
+      int n_near = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-          unsure |= (key[v] > -INFINITY) & !(key[v] < near) & !((l[v] == last.logit) & (b[v] == lb));
+      for (int v = 0; v < V; ++v) n_near += !(key[v] < near);
+      // beside the chosen
+      if (__any(last.idx >= 0 && group_sum<L>((float)n_near) > (kept ? (float)k : 0.0f))) {
+        const float lb = last.idx >= 0 ? bias[last.idx] : 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)  // not chosen, not clearly below, and not equal in all
+          unsure |= (last.idx >= 0) & (key[v] > -INFINITY) & !(key[v] < near) &
+                    (!kept | (key[v] < last.key) | ((key[v] == last.key) & (lane * V + v > last.idx))) &
+                    !((l[v] == last.logit) & (b[v] == lb));
       }
       if (__any(unsure)) {
         double z = 1.0, key64[V];
