@@ -161,16 +161,27 @@ __device__ __forceinline__ float packed_logit(uint32_t key) {
   return __uint_as_float((ord & 0x8000u ? ord ^ 0x8000u : ~ord & 0xFFFFu) << 16);
 }
 
-// What a round has found, by slot.
+// What a round has found, by slot of a group.
 struct Choice {
   int idx;
   float logit, key;
 };
+template <int kSlots>
+struct Choices {
+  int idx[kSlots];
+  float logit[kSlots], key[kSlots];
+  __device__ __forceinline__ void put(int i, const Choice& c) {
+    idx[i] = c.idx;
+    logit[i] = c.logit;
+    key[i] = c.key;
+  }
+  __device__ __forceinline__ Choice get(int i) const { return {idx[i], logit[i], key[i]}; }
+};
 
 // k rounds over keys of type K (-inf: never chosen): the largest of the group, the lowest lane that has it, its
 // lowest expert.  Slot j of `out` is written by the lane that held it; chosen keys become -inf.
-template <int L, int V, typename K>
-__device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], int k, Choice* out) {
+template <int L, int V, typename K, typename Out>
+__device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], int k, Out& out) {
   const int lane = threadIdx.x & (L - 1), base = threadIdx.x & 63 & ~(L - 1);
   for (int j = 0; j < k; ++j) {
     K best = key[0];
@@ -198,7 +209,7 @@ __device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], 
       key[v] = hit ? (K)-INFINITY : key[v];
       mine = mine && !hit;
     }
-    if (lane == win) out[j] = {top > -INFINITY ? lane * V + at : -1, logit, (float)top};
+    if (lane == win) out.put(j, {top > -INFINITY ? lane * V + at : -1, logit, (float)top});
   }
 }
 
@@ -233,42 +244,43 @@ __device__ __forceinline__ int row_inclusive_sum(int v) {
   v += (int)dpp<0x118>((uint32_t)v);
   return v;
 }
-template <int V>
-__device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float (&l)[V], int k, Choice* out) {
+template <int V, typename Out>
+__device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float (&l)[V], int k, Out& out) {
   const int lane = threadIdx.x & 15;
   float best = key[0];
 #pragma unroll
   for (int v = 1; v < V; ++v) best = fmaxf(best, key[v]);
-  const float bound = -group_max<16>(count_larger<1>(best, 0) < k ? -best : -INFINITY);
+  // at least the lowest finite number: a key of -inf is no candidate
+  const float bound = fmaxf(-group_max<16>(count_larger<1>(best, 0) < k ? -best : -INFINITY), -3.402823466e38f);
   int n = 0;
 #pragma unroll
-  for (int v = 0; v < V; ++v) n += (key[v] >= bound) & (key[v] > -INFINITY);
+  for (int v = 0; v < V; ++v) n += key[v] >= bound;
   const int end = row_inclusive_sum(n), total = (int)dpp<0x15F>((uint32_t)end);
   if (__any(total > 32)) return false;
   int at = end - n;
 #pragma unroll
   for (int v = 0; v < V; ++v)
-    if ((key[v] >= bound) & (key[v] > -INFINITY)) out[at++] = {lane * V + v, l[v], key[v]};
+    if (key[v] >= bound) out.put(at++, {lane * V + v, l[v], key[v]});
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   Choice c = {-1, -INFINITY, -INFINITY}, d = c;
-  if (lane < total) c = out[lane];
+  if (lane < total) c = out.get(lane);
   int rank = count_before<0, false>(c.key, c.key, lane, 0);
   if (__any(total > 16)) {
-    if (lane + 16 < total) d = out[lane + 16];
+    if (lane + 16 < total) d = out.get(lane + 16);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     // every value of the first sixteen stands before an equal one of the second
     rank += count_before<0, true>(d.key, c.key, -1, 0);
     const int rank_d = count_before<0, false>(d.key, d.key, lane, 0) + count_before<0, true>(c.key, d.key, 16, 0);
-    if (rank_d < k) out[rank_d] = d;
+    if (rank_d < k) out.put(rank_d, d);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (rank < k) out[rank] = c;
+  if (rank < k) out.put(rank, c);
   return true;
 }
 
 // True if the chosen keys are still there (the rounds leave -inf in their place).
-template <int L, int V>
-__device__ __forceinline__ bool choose(float (&key)[V], const float (&l)[V], int k, Choice* out) {
+template <int L, int V, typename Out>
+__device__ __forceinline__ bool choose(float (&key)[V], const float (&l)[V], int k, Out& out) {
   if constexpr (L == 16 && V > 1) {
     if (k <= 8 && choose_ranked<V>(key, l, k, out)) return true;
   }
@@ -283,9 +295,9 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
   constexpr bool kPacked = sizeof(X) == 2 && !kBias;
   constexpr bool kFull = !kSigmoid && (kBias || !kNormalize);  // the softmax over all experts is needed
   constexpr int kFound = L == 16 ? 32 : 64;  // slots a group: k, or the candidates for them
-  __shared__ Choice found[kPacked ? 1 : kThreads / L * kFound];
+  __shared__ Choices<kFound> found[kPacked ? 1 : kThreads / L];
   const int lane = threadIdx.x & (L - 1);
-  Choice* const mine = &found[kPacked ? 0 : threadIdx.x / L * kFound];
+  Choices<kFound>& mine = found[kPacked ? 0 : threadIdx.x / L];
   const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
   if (t >= T) return;  // whole groups of L lanes
   X raw[V], missing;
@@ -348,11 +360,11 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
       const float err = kSigmoid ? 0x1p-19f : 0x1p-16f * inv;
       bool unsure = false;
       if (lane + 1 < k) {
-        const Choice a = mine[lane], n = mine[lane + 1];
+        const Choice a = mine.get(lane), n = mine.get(lane + 1);
         if (n.idx >= 0 && !(a.key - n.key > err + 0x1p-21f * fabsf(a.key)))
           unsure = !(a.logit == n.logit && bias[a.idx] == bias[n.idx]);
       }
-      const Choice last = mine[k - 1];
+      const Choice last = mine.get(k - 1);
       const float near = last.key - (err + 0x1p-21f * fabsf(last.key));
       int n_near = 0;
 #pragma unroll
@@ -388,7 +400,7 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (lane < k) c = mine[lane];
+    if (lane < k) c = mine.get(lane);
   }
   float w = 0.0f;
   if (kNormalize) {
