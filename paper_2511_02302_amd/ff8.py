@@ -428,73 +428,112 @@ def ff8_unpermute(y_perm, row_map, row_w, y, stream=None):
 
 SCORES = {"softmax": 0, "sigmoid": 1}
 
+_NO_DEVICE = -2
+_get_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
-def _here(stream, *tensors):
-    """Every tensor (checked to be a device tensor) lies on the current device, whose stream the call goes to."""
-    dev = torch._C._cuda_getDevice()
-    if stream is not None and stream.device.index != dev:
+
+def _target(stream):
+    """(device, raw stream) of a call: the current device, whose tensors and streams alone it takes."""
+    if not torch.cuda.is_initialized():
+        return _NO_DEVICE, None  # there can be no device tensor: _call refuses behind the other checks
+    dev = _get_device()
+    if stream is None:
+        return dev, _raw_stream(dev)
+    if stream.device.index != dev:
         raise ValueError(f"the stream is on {stream.device}, the current device is cuda:{dev}")
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+    return dev, stream.cuda_stream
+
+
+def _refuse(t, dtype, name, dev):
+    if dev == _NO_DEVICE and t.dtype is dtype:
+        return None
+    _ptr(t, dtype, name)
+    raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+
+
+def _call(name, dev, *args):
+    if dev == _NO_DEVICE:
+        raise ValueError(f"{name}: every tensor must be a device tensor")
+    status = getattr(load(), name)(*args)
+    if status != 0:
+        _check(status, name)
+
+
+def _at(t, dtype, shape, name, dev):
+    """data_ptr of a tensor of this type and shape on this device.  (One test for all that is right, as small
+    calls are bound by the host; what is wrong is found by the checks that name it.)"""
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.shape == shape:
+        return t.data_ptr()
+    _shape(t, shape, name)
+    return _refuse(t, dtype, name, dev)
+
+
+def _at_n(t, dtype, n, name, dev):
+    """The same for a tensor of n elements in any shape, or None."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.numel() == n:
+        return t.data_ptr()
+    _numel(t, n, name)
+    return _refuse(t, dtype, name, dev)
+
+
+def _at_ws(t, dev):
+    if t is None:
+        return None, 0
+    if dev != _NO_DEVICE and not (t.get_device() == dev and t.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor on the current device")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _router(name, logits, score):
-    T, E = logits.shape
     if score not in SCORES:
         raise ValueError(f"score must be one of {sorted(SCORES)}")
     if logits.dtype is _bf16:
-        return T, E, name + "_bf16", _bf16
+        return name + "_bf16", _bf16
     if logits.dtype is _f32:
-        return T, E, name, _f32
+        return name, _f32
     raise TypeError(f"logits must be float32 or bfloat16, got {logits.dtype}")
 
 
 def ff8_router_topk(logits, topk_idx, probs, bias=None, score="softmax", normalize=False, scale=1.0, stream=None):
     """Experts and routing weights of each token; k is topk_idx's width, score "softmax" or "sigmoid"."""
-    T, E, name, dt = _router("ff8_router_topk", logits, score)
+    T, E = logits.shape
     k = topk_idx.shape[1]
-    _shape(topk_idx, (T, k), "topk_idx"); _shape(probs, (T, k), "probs"); _numel(bias, E, "bias")
-    args = [_ptr(logits, dt, "logits", 2), _ptr(bias, _f32, "bias"), T, E, k, SCORES[score], int(bool(normalize)),
-            float(scale), _ptr(topk_idx, _i32, "topk_idx", 2), _ptr(probs, _f32, "probs", 2)]
-    _here(stream, logits, bias, topk_idx, probs)
-    _check(getattr(load(), name)(*args, _stream(stream)), name)
+    name, dt = _router("ff8_router_topk", logits, score)
+    dev, st = _target(stream)
+    _call(name, dev,
+          _at(logits, dt, (T, E), "logits", dev), _at_n(bias, _f32, E, "bias", dev), T, E, k, SCORES[score],
+          int(bool(normalize)), scale, _at(topk_idx, _i32, (T, k), "topk_idx", dev), _at(probs, _f32, (T, k), "probs", dev),
+          st)
 
 
 def ff8_router_topk_bwd(logits, topk_idx, dprobs, dlogits, score="softmax", normalize=False, scale=1.0, stream=None):
     """dlogits (of the logits' type) from the gradient of the routing weights."""
-    T, E, name, dt = _router("ff8_router_topk_bwd", logits, score)
+    T, E = logits.shape
     k = topk_idx.shape[1]
-    _shape(topk_idx, (T, k), "topk_idx"); _shape(dprobs, (T, k), "dprobs"); _shape(dlogits, (T, E), "dlogits")
-    args = [_ptr(logits, dt, "logits", 2), _ptr(topk_idx, _i32, "topk_idx", 2), _ptr(dprobs, _f32, "dprobs", 2), T, E,
-            k, SCORES[score], int(bool(normalize)), float(scale), _ptr(dlogits, dt, "dlogits", 2)]
-    _here(stream, logits, topk_idx, dprobs, dlogits)
-    _check(getattr(load(), name)(*args, _stream(stream)), name)
+    name, dt = _router("ff8_router_topk_bwd", logits, score)
+    dev, st = _target(stream)
+    _call(name, dev,
+          _at(logits, dt, (T, E), "logits", dev), _at(topk_idx, _i32, (T, k), "topk_idx", dev),
+          _at(dprobs, _f32, (T, k), "dprobs", dev), T, E, k, SCORES[score], int(bool(normalize)), scale,
+          _at(dlogits, dt, (T, E), "dlogits", dev), st)
 
 
-def _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row):
-    _numel(topk_idx, T * k, "topk_idx"); _numel(row_map, T * k, "row_map")
-    _numel(offsets, E + 1, "offsets"); _numel(src_row, M_cap, "src_row")
-    return (_ptr(topk_idx, _i32, "topk_idx"), _ptr(row_map, _i32, "row_map"), _ptr(offsets, _i32, "offsets"),
-            _ptr(src_row, _i32, "src_row"))
-
-
-def _ws(workspace):
-    if workspace is None:
-        return None, 0
-    if not (workspace.is_cuda and workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous device tensor")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+def _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row, dev):
+    return (_at_n(topk_idx, _i32, T * k, "topk_idx", dev), _at_n(row_map, _i32, T * k, "row_map", dev),
+            _at_n(offsets, _i32, E + 1, "offsets", dev), _at_n(src_row, _i32, M_cap, "src_row", dev))
 
 
 def ff8_route(topk_idx, E, row_map, offsets, src_row, workspace, align=128, stream=None):
     """The routing maps alone (as the permutes build them); M_cap is src_row's length."""
     T, k = topk_idx.shape
     M_cap = src_row.numel()
-    idx, rm, off, src = _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row)
-    ws, n = _ws(workspace)
-    _here(stream, topk_idx, row_map, offsets, src_row, workspace)
-    _check(load().ff8_route(idx, T, k, E, rm, off, src, M_cap, ws, n, int(align), _stream(stream)), "ff8_route")
+    dev, st = _target(stream)
+    idx, rm, off, src = _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row, dev)
+    ws, n = _at_ws(workspace, dev)
+    _call("ff8_route", dev, idx, T, k, E, rm, off, src, M_cap, ws, n, int(align), st)
 
 
 def ff8_permute_bf16(x, k, E, topk_idx, reuse_map, row_map, offsets, src_row, out, workspace=None, align=128,
@@ -502,13 +541,11 @@ def ff8_permute_bf16(x, k, E, topk_idx, reuse_map, row_map, offsets, src_row, ou
     """bf16 rows sorted by expert, groups padded with zero rows; maps as ff8_permute_quant's."""
     T, H = x.shape
     M_cap = out.shape[0]
-    _shape(out, (M_cap, H), "out")
-    idx, rm, off, src = _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row)
-    ws, n = _ws(workspace)
-    args = [_ptr(x, _bf16, "x", 2), T, H, k, E, idx, int(reuse_map), rm, off, src, M_cap, _ptr(out, _bf16, "out", 2),
-            ws, n, int(align)]
-    _here(stream, x, topk_idx, row_map, offsets, src_row, out, workspace)
-    _check(load().ff8_permute_bf16(*args, _stream(stream)), "ff8_permute_bf16")
+    dev, st = _target(stream)
+    idx, rm, off, src = _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row, dev)
+    ws, n = _at_ws(workspace, dev)
+    _call("ff8_permute_bf16", dev, _at(x, _bf16, (T, H), "x", dev), T, H, k, E, idx, int(reuse_map), rm, off, src, M_cap,
+          _at(out, _bf16, (M_cap, H), "out", dev), ws, n, int(align), st)
 
 
 def ff8_permute_fp8(xq, xs, k, E, topk_idx, reuse_map, row_map, offsets, src_row, q, s, workspace=None, align=128,
@@ -516,38 +553,36 @@ def ff8_permute_fp8(xq, xs, k, E, topk_idx, reuse_map, row_map, offsets, src_row
     """Rows that are e4m3 already, with their 1x128 scales (float32 or UE8M0), sorted by expert."""
     T, H = xq.shape
     M_cap = q.shape[0]
-    _shape(xs, (T, H // 128), "xs"); _shape(q, (M_cap, H), "q"); _shape(s, (M_cap, H // 128), "s")
     sd, sfx = _scale_kind(xs, s)
-    idx, rm, off, src = _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row)
-    ws, n = _ws(workspace)
     name = "ff8_permute_fp8" + sfx
-    args = [_ptr(xq, _u8, "xq", 2), _ptr(xs, sd, "xs", 2), T, H, k, E, idx, int(reuse_map), rm, off, src, M_cap,
-            _ptr(q, _u8, "q", 2), _ptr(s, sd, "s", 2), ws, n, int(align)]
-    _here(stream, xq, xs, topk_idx, row_map, offsets, src_row, q, s, workspace)
-    _check(getattr(load(), name)(*args, _stream(stream)), name)
+    dev, st = _target(stream)
+    idx, rm, off, src = _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row, dev)
+    ws, n = _at_ws(workspace, dev)
+    _call(name, dev,
+          _at(xq, _u8, (T, H), "xq", dev), _at(xs, sd, (T, H // 128), "xs", dev), T, H, k, E, idx, int(reuse_map), rm, off,
+          src, M_cap, _at(q, _u8, (M_cap, H), "q", dev), _at(s, sd, (M_cap, H // 128), "s", dev), ws, n, int(align), st)
 
 
 def ff8_unpermute_bwd(dy, row_w, k, E, row_map, offsets, src_row, dy_perm, y_perm=None, dprobs=None, stream=None):
     """The gradient of the weighted return: dy_perm, and with y_perm also the routing weights' dprobs."""
     T, H = dy.shape
     M_cap = dy_perm.shape[0]
-    _numel(row_w, T * k, "row_w"); _numel(dprobs, T * k, "dprobs")
-    _shape(dy_perm, (M_cap, H), "dy_perm"); _shape(y_perm, (M_cap, H), "y_perm")
-    _, rm, off, src = _maps(T, k, E, M_cap, None, row_map, offsets, src_row)
-    args = [_ptr(dy, _bf16, "dy", 2), _ptr(row_w, _f32, "row_w"), T, H, k, E, rm, off, src, M_cap,
-            _ptr(dy_perm, _bf16, "dy_perm", 2), _ptr(y_perm, _bf16, "y_perm", 2), _ptr(dprobs, _f32, "dprobs")]
-    _here(stream, dy, row_w, row_map, offsets, src_row, dy_perm, y_perm, dprobs)
-    _check(load().ff8_unpermute_bwd(*args, _stream(stream)), "ff8_unpermute_bwd")
+    dev, st = _target(stream)
+    _, rm, off, src = _maps(T, k, E, M_cap, None, row_map, offsets, src_row, dev)
+    _call("ff8_unpermute_bwd", dev,
+          _at(dy, _bf16, (T, H), "dy", dev), _at_n(row_w, _f32, T * k, "row_w", dev), T, H, k, E, rm, off, src, M_cap,
+          _at(dy_perm, _bf16, (M_cap, H), "dy_perm", dev),
+          None if y_perm is None else _at(y_perm, _bf16, (M_cap, H), "y_perm", dev), _at_n(dprobs, _f32, T * k, "dprobs", dev),
+          st)
 
 
 def ff8_quant_mxfp4(w, q, s, stream=None):
     """w [..., K] bf16 -> q [..., K // 2] (two e2m1 codes a byte), s [..., K // 32] (UE8M0 bytes)."""
     *lead, K = w.shape
     rows = w.numel() // K if K else 0
-    _shape(q, (*lead, K // 2), "q"); _shape(s, (*lead, K // 32), "s")
-    args = [_ptr(w, _bf16, "w"), rows, K, _ptr(q, _u8, "q"), _ptr(s, _u8, "s")]
-    _here(stream, w, q, s)
-    _check(load().ff8_quant_mxfp4(*args, _stream(stream)), "ff8_quant_mxfp4")
+    dev, st = _target(stream)
+    _call("ff8_quant_mxfp4", dev, _at(w, _bf16, (*lead, K), "w", dev), rows, K, _at(q, _u8, (*lead, K // 2), "q", dev),
+          _at(s, _u8, (*lead, K // 32), "s", dev), st)
 
 
 def ff8_pack_mxfp4(q, s, tq, ts, stream=None):
@@ -555,26 +590,24 @@ def ff8_pack_mxfp4(q, s, tq, ts, stream=None):
     (ordered [E, N // 32, K // 128, 64, 2], any shape)."""
     E, N, half = q.shape
     K = 2 * half
-    _shape(s, (E, N, K // 32), "s"); _shape(tq, (E, N // 16, K // 128, 64, 16), "tq")
-    _numel(ts, E * N * K // 32, "ts")
-    args = [_ptr(q, _u8, "q", 3), _ptr(s, _u8, "s", 3), E * N, K, _ptr(tq, _u8, "tq"), _ptr(ts, _u8, "ts")]
-    _here(stream, q, s, tq, ts)
-    _check(load().ff8_pack_mxfp4(*args, _stream(stream)), "ff8_pack_mxfp4")
+    dev, st = _target(stream)
+    _call("ff8_pack_mxfp4", dev,
+          _at(q, _u8, (E, N, half), "q", dev), _at(s, _u8, (E, N, K // 32), "s", dev), E * N, K,
+          _at(tq, _u8, (E, N // 16, K // 128, 64, 16), "tq", dev), _at_n(ts, _u8, E * N * K // 32, "ts", dev), st)
 
 
-def _gemv_mxfp4(name, cols, x, tq, ts, offsets, out, src_row, top_k, stream):
+def _gemv_mxfp4(name, parts, x, tq, ts, offsets, out, src_row, top_k, stream):
     x_rows, K = x.shape
     E, nt, _, _, _ = tq.shape
-    N = 16 * nt
-    M_cap = out.shape[0]
-    _shape(tq, (E, nt, K // 128, 64, 16), "tq"); _numel(ts, E * N * K // 32, "ts")
-    _numel(offsets, E + 1, "offsets"); _numel(src_row, M_cap, "src_row"); _shape(out, (M_cap, N // cols), "out")
-    if N % cols:
+    N, M_cap = 16 * nt, out.shape[0]
+    if N % parts:
         raise ValueError("tq must have shape (E, 2I // 16, K // 128, 64, 16)")
-    args = [_ptr(x, _bf16, "x", 2), x_rows, _ptr(tq, _u8, "tq"), _ptr(ts, _u8, "ts"), _ptr(offsets, _i32, "offsets"), E,
-            _ptr(src_row, _i32, "src_row"), int(top_k), M_cap, N // cols, K, _ptr(out, _bf16, "out", 2)]
-    _here(stream, x, tq, ts, offsets, out, src_row)
-    _check(getattr(load(), name)(*args, _stream(stream)), name)
+    dev, st = _target(stream)
+    _call(name, dev,
+          _at(x, _bf16, (x_rows, K), "x", dev), x_rows, _at(tq, _u8, (E, nt, K // 128, 64, 16), "tq", dev),
+          _at_n(ts, _u8, E * N * K // 32, "ts", dev), _at_n(offsets, _i32, E + 1, "offsets", dev), E,
+          _at_n(src_row, _i32, M_cap, "src_row", dev), int(top_k), M_cap, N // parts, K,
+          _at(out, _bf16, (M_cap, N // parts), "out", dev), st)
 
 
 def ff8_grouped_gemv_mxfp4(x, tq, ts, offsets, out, src_row=None, top_k=0, stream=None):
