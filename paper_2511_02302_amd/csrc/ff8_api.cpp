@@ -431,17 +431,12 @@ int ff8_route(const int32_t* topk_idx, int64_t T, int k, int E, int32_t* row_map
 int ff8_permute_bf16(const ff8_bf16* x, int64_t T, int64_t H, int k, int E, const int32_t* topk_idx, int reuse_map,
                      int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap, ff8_bf16* out,
                      void* workspace, size_t ws_bytes, int align, void* stream) {
-  int rc = permute_validate(__func__, x, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, out, out,
-                            workspace, ws_bytes, align, true);
+  const int rc = permute_validate(__func__, x, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, out,
+                                  out, workspace, ws_bytes, align, true);
   if (rc != FF8_OK) return rc;
   REQUIRE_ALIGNED(x); REQUIRE_ALIGNED(out);
-  if (!reuse_map) {
-    rc = hip_status(ff8::launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace,
-                                      as_stream(stream)),
-                    __func__);
-    if (rc != FF8_OK) return rc;
-  }
-  return hip_status(ff8::launch_permute_bf16(x, T, H, k, E, row_map, offsets, src_row, M_cap, out, as_stream(stream)),
+  return hip_status(ff8::launch_permute_bf16(x, T, H, k, E, reuse_map ? nullptr : topk_idx, align, workspace, row_map,
+                                             offsets, src_row, M_cap, out, as_stream(stream)),
                     __func__);
 }
 
@@ -451,17 +446,15 @@ template <typename SC>
 static int permute_fp8(const char* fn, const ff8_e4m3* xq, const SC* xs, int64_t T, int64_t H, int k, int E,
                        const int32_t* topk_idx, int reuse_map, int32_t* row_map, int32_t* offsets, int32_t* src_row,
                        int64_t M_cap, ff8_e4m3* q, SC* s, void* workspace, size_t ws_bytes, int align, hipStream_t st) {
-  int rc = permute_validate(fn, xq, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, q, s, workspace,
-                            ws_bytes, align, true);
+  const int rc = permute_validate(fn, xq, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, q, s,
+                                  workspace, ws_bytes, align, true);
   if (rc != FF8_OK) return rc;
   if (T > 0 && !xs) return fail(FF8_ERR_NULL, "%s: xs is NULL", fn);
   if ((reinterpret_cast<uintptr_t>(xq) | reinterpret_cast<uintptr_t>(q)) % 16 != 0)
     return fail(FF8_ERR_ARG, "%s: xq and q must be 16-byte aligned", fn);
-  if (!reuse_map) {
-    rc = hip_status(ff8::launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace, st), fn);
-    if (rc != FF8_OK) return rc;
-  }
-  return hip_status(ff8::launch_permute_fp8(xq, xs, T, H, k, E, row_map, offsets, src_row, M_cap, q, s, st), fn);
+  return hip_status(ff8::launch_permute_fp8(xq, xs, T, H, k, E, reuse_map ? nullptr : topk_idx, align, workspace, row_map,
+                                            offsets, src_row, M_cap, q, s, st),
+                    fn);
 }
 
 // Common to the two 4-bit products; N counts weight rows.

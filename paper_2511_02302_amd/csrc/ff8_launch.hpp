@@ -76,17 +76,17 @@ hipError_t launch_router_topk_bwd(const float* logits, const int32_t* idx, const
 hipError_t launch_router_topk_bwd(const uint16_t* logits, const int32_t* idx, const float* dprobs, int64_t T, int E,
                                   int k, bool sig, bool norm, float scale, uint16_t* dlogits, hipStream_t st);
 
-// Rows moved without a cast, by maps that are already built, and the gradient of the weighted return
-// (y_perm and dprobs both NULL: dy_perm alone).
-hipError_t launch_permute_bf16(const uint16_t* x, int64_t T, int64_t H, int k, int E, const int32_t* row_map,
-                               const int32_t* offsets, const int32_t* src_row, int64_t M_cap, uint16_t* out,
-                               hipStream_t st);
+// Rows moved without a cast, with their routing maps built from topk_idx, or by maps that are there (topk_idx NULL);
+// and the gradient of the weighted return (y_perm and dprobs both NULL: dy_perm alone).
+hipError_t launch_permute_bf16(const uint16_t* x, int64_t T, int64_t H, int k, int E, const int32_t* topk_idx, int align,
+                               void* workspace, int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap,
+                               uint16_t* out, hipStream_t st);
 hipError_t launch_permute_fp8(const uint8_t* xq, const float* xs, int64_t T, int64_t H, int k, int E,
-                              const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
-                              uint8_t* q, float* s, hipStream_t st);
+                              const int32_t* topk_idx, int align, void* workspace, int32_t* row_map, int32_t* offsets,
+                              int32_t* src_row, int64_t M_cap, uint8_t* q, float* s, hipStream_t st);
 hipError_t launch_permute_fp8(const uint8_t* xq, const e8m0_t* xs, int64_t T, int64_t H, int k, int E,
-                              const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
-                              uint8_t* q, e8m0_t* s, hipStream_t st);
+                              const int32_t* topk_idx, int align, void* workspace, int32_t* row_map, int32_t* offsets,
+                              int32_t* src_row, int64_t M_cap, uint8_t* q, e8m0_t* s, hipStream_t st);
 hipError_t launch_unpermute_bwd(const uint16_t* dy, const float* row_w, int64_t T, int64_t H, int k, int E,
                                 const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
                                 uint16_t* dy_perm, const uint16_t* y_perm, float* dprobs, hipStream_t st);

@@ -26,9 +26,34 @@ namespace {
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kPieces = 8;  // 16-byte pieces that a lane has in flight
 
+// One wave: row r becomes token t's row, or a row of zeros (scales 2^-126).  row16: 16-byte pieces of a row; n_s:
+// its scales (0 for bf16 rows).
+template <typename S>
+__device__ __forceinline__ void move_row(const u32x4* __restrict__ x, const S* __restrict__ s, int64_t t, int64_t r,
+                                         int lane, int64_t row16, int n_s, u32x4* __restrict__ out,
+                                         S* __restrict__ s_out) {
+  for (int64_t c0 = lane; c0 < row16; c0 += 64 * kPieces) {
+    u32x4 v[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (c0 + 64 * i < row16) v[i] = ld16(x + t * row16 + c0 + 64 * i);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (c0 + 64 * i < row16) stnt16(out + r * row16 + c0 + 64 * i, v[i]);
+  }
+  for (int c = lane; c < n_s; c += 64) s_out[r * n_s + c] = s[t * n_s + c];
+}
+template <typename S>
+__device__ __forceinline__ void clear_row(int64_t r, int lane, int64_t row16, int n_s, u32x4* __restrict__ out,
+                                          S* __restrict__ s_out) {
+  const u32x4 z = {0u, 0u, 0u, 0u};
+  for (int64_t c = lane; c < row16; c += 64) stnt16(out + r * row16 + c, z);
+  for (int c = lane; c < n_s; c += 64) put_scale(&s_out[r * n_s + c], kTMin);
+}
+
 // Zeros in the padding rows (src_row < 0) of expert e's group: fewer than 128, all among the group's last 128.
 // Their numbers are collected in LDS first (two loads a lane instead of one before every row), then each wave
-// takes every eighth.  row16: 16-byte pieces of a row; n_s: its scales (0 for bf16 rows).
+// takes every eighth.
 template <typename S>
 __device__ __forceinline__ void pad_rows(int e, const int32_t* __restrict__ offsets, const int32_t* __restrict__ src_row,
                                          int64_t M_cap, int64_t row16, int n_s, u32x4* __restrict__ out,
@@ -51,12 +76,7 @@ __device__ __forceinline__ void pad_rows(int e, const int32_t* __restrict__ offs
     if (lane == 0) n_rows = n;
   }
   __syncthreads();
-  const u32x4 z = {0u, 0u, 0u, 0u};
-  for (int i = threadIdx.x >> 6; i < n_rows; i += kWaves) {
-    const int64_t r = r0 + rows[i];
-    for (int64_t c = lane; c < row16; c += 64) stnt16(out + r * row16 + c, z);
-    for (int c = lane; c < n_s; c += 64) put_scale(&s_out[r * n_s + c], kTMin);
-  }
+  for (int i = threadIdx.x >> 6; i < n_rows; i += kWaves) clear_row<S>(r0 + rows[i], lane, row16, n_s, out, s_out);
 }
 
 // The (token, slot) pair of a wave behind the E padding workgroups; the same for all its lanes.
@@ -78,17 +98,83 @@ __global__ __launch_bounds__(kThreads) void sort_rows_kernel(const u32x4* __rest
   const int p = pair_of_wave(E), lane = threadIdx.x & 63;
   if (p >= n_pairs) return;
   const int64_t t = p / k, r = row_map[p];
-  if (r < 0 || r >= M_cap) return;
-  for (int64_t c0 = lane; c0 < row16; c0 += 64 * kPieces) {
-    u32x4 v[kPieces];
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i)
-      if (c0 + 64 * i < row16) v[i] = ld16(x + t * row16 + c0 + 64 * i);
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i)
-      if (c0 + 64 * i < row16) stnt16(out + r * row16 + c0 + 64 * i, v[i]);
+  if (r >= 0 && r < M_cap) move_row<S>(x, s, t, r, lane, row16, n_s, out, s_out);
+}
+
+// Routing and rows in one launch, for routings that every workgroup can count by itself (T * k <= 4096): a
+// workgroup takes eight (token, slot) pairs, counts all the pairs of each expert and those before its own, and so
+// knows the group offsets and its rows.  Behind those, one workgroup an expert fills the group's padding.  Integer
+// LDS atomics: the counts do not depend on order.  Against the routing in launches of its own (us): 1024 tokens x
+// 256 columns, 8 experts, k = 2 6.9 / 11.4; 512 x 7168, 64 experts, k = 8 17 / 26, with 128-row padding 29 / 38; 4096 x
+// 256, 1024 experts, k = 1 10.4 / 12.7.
+constexpr int kMaxExperts = 1024, kMaxPairs = 4096;
+template <typename S>
+__global__ __launch_bounds__(kThreads) void route_sort_kernel(const u32x4* __restrict__ x, const S* __restrict__ s,
+                                                              const int32_t* __restrict__ topk_idx, int n_pairs, int k,
+                                                              int E, int align, int64_t row16, int n_s, int64_t M_cap,
+                                                              int32_t* __restrict__ row_map,
+                                                              int32_t* __restrict__ offsets,
+                                                              int32_t* __restrict__ src_row, u32x4* __restrict__ out,
+                                                              S* __restrict__ s_out) {
+  __shared__ unsigned count[kMaxExperts];  // pairs of an expert, and those before the workgroup's in the high half
+  __shared__ int start[kMaxExperts + 1], wave_sum[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n_sort = (n_pairs + kWaves - 1) / kWaves, pad = (int)blockIdx.x - n_sort;  // pad: the expert, or below 0
+  const int p0 = (int)blockIdx.x * kWaves;
+  for (int e = tid; e < E; e += kThreads) count[e] = 0;
+  __syncthreads();
+  for (int i = tid; i < n_pairs; i += kThreads) {
+    const int e = topk_idx[i];
+    if (e >= 0 && e < E) atomicAdd(&count[e], i < p0 ? 0x10001u : 1u);
   }
-  for (int c = lane; c < n_s; c += 64) s_out[r * n_s + c] = s[t * n_s + c];
+  __syncthreads();
+  // group offsets: two experts a thread, scanned over the wave and the waves
+  static_assert(2 * kThreads >= kMaxExperts, "two experts a thread");
+  int rows[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int e = 2 * tid + h, n = e < E ? (int)(count[e] & 0xFFFFu) : 0;
+    rows[h] = (n + align - 1) / align * align;
+  }
+  int end = rows[0] + rows[1];
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(end, d);
+    if (lane >= d) end += u;
+  }
+  if (lane == 63) wave_sum[wave] = end;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) end += wave_sum[w];
+  if (tid == 0) start[0] = 0;
+  if (2 * tid < E) start[2 * tid + 1] = end - rows[1];
+  if (2 * tid + 1 < E) start[2 * tid + 2] = end;
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int e = tid; e <= E; e += kThreads) offsets[e] = start[e];
+  if (pad < 0) {
+    const int p = __builtin_amdgcn_readfirstlane(p0 + wave);
+    if (p >= n_pairs) return;
+    const int mine = p0 + lane < n_pairs && lane < kWaves ? topk_idx[p0 + lane] : -1;
+    const int e = __builtin_amdgcn_readlane(mine, wave);
+    if (e < 0 || e >= E) {
+      if (lane == 0) row_map[p] = -1;
+      return;
+    }
+    const unsigned long long before = __ballot(mine == e && lane < wave);
+    const int64_t r = start[e] + (int)(count[e] >> 16) + __popcll(before);
+    if (r >= M_cap) return;
+    if (lane == 0) {
+      row_map[p] = (int)r;
+      src_row[r] = p;
+    }
+    move_row<S>(x, s, p / k, r, lane, row16, n_s, out, s_out);
+  } else {
+    const int64_t r1 = start[pad + 1] < M_cap ? start[pad + 1] : M_cap;
+    for (int64_t r = start[pad] + (int)(count[pad] & 0xFFFFu) + wave; r < r1; r += kWaves) {
+      if (lane == 0) src_row[r] = -1;
+      clear_row<S>(r, lane, row16, n_s, out, s_out);
+    }
+  }
 }
 
 // Sum of a dot product, fixed order: a lane's products in column order, then a butterfly over the wave.
@@ -141,32 +227,47 @@ __global__ __launch_bounds__(kThreads) void return_bwd_kernel(
 
 unsigned grid_of(int64_t n_pairs, int E) { return (unsigned)(E + (n_pairs + kWaves - 1) / kWaves); }
 
+// With topk_idx the routing maps are built too.
 template <typename S>
-hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_s, int k, int E, const int32_t* row_map,
-                     const int32_t* offsets, const int32_t* src_row, int64_t M_cap, void* out, S* s_out,
-                     hipStream_t st) {
-  sort_rows_kernel<S><<<grid_of(T * k, E), kThreads, 0, st>>>(static_cast<const u32x4*>(x), s, row16, n_s, (int)(T * k),
-                                                              k, E, row_map, offsets, src_row, M_cap,
-                                                              static_cast<u32x4*>(out), s_out);
+hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_s, int k, int E, const int32_t* topk_idx,
+                     int align, void* workspace, int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap,
+                     void* out, S* s_out, hipStream_t st) {
+  const u32x4* const in = static_cast<const u32x4*>(x);
+  u32x4* const to = static_cast<u32x4*>(out);
+  const int64_t n_pairs = T * k;
+  if (topk_idx || T == 0) {
+    if (n_pairs <= kMaxPairs) {
+      route_sort_kernel<S><<<grid_of(n_pairs, E), kThreads, 0, st>>>(in, s, topk_idx, (int)n_pairs, k, E, align, row16,
+                                                                     n_s, M_cap, row_map, offsets, src_row, to, s_out);
+      return hipGetLastError();
+    }
+    const hipError_t e = launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace, st);
+    if (e != hipSuccess) return e;
+  }
+  sort_rows_kernel<S><<<grid_of(n_pairs, E), kThreads, 0, st>>>(in, s, row16, n_s, (int)n_pairs, k, E, row_map, offsets,
+                                                                src_row, M_cap, to, s_out);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_permute_bf16(const uint16_t* x, int64_t T, int64_t H, int k, int E, const int32_t* row_map,
-                               const int32_t* offsets, const int32_t* src_row, int64_t M_cap, uint16_t* out,
-                               hipStream_t st) {
-  return sort_rows<e8m0_t>(x, nullptr, T, H / 8, 0, k, E, row_map, offsets, src_row, M_cap, out, nullptr, st);
+hipError_t launch_permute_bf16(const uint16_t* x, int64_t T, int64_t H, int k, int E, const int32_t* topk_idx, int align,
+                               void* workspace, int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap,
+                               uint16_t* out, hipStream_t st) {
+  return sort_rows<e8m0_t>(x, nullptr, T, H / 8, 0, k, E, topk_idx, align, workspace, row_map, offsets, src_row, M_cap,
+                           out, nullptr, st);
 }
 hipError_t launch_permute_fp8(const uint8_t* xq, const float* xs, int64_t T, int64_t H, int k, int E,
-                              const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
-                              uint8_t* q, float* s, hipStream_t st) {
-  return sort_rows(xq, xs, T, H / 16, (int)(H / kTile), k, E, row_map, offsets, src_row, M_cap, q, s, st);
+                              const int32_t* topk_idx, int align, void* workspace, int32_t* row_map, int32_t* offsets,
+                              int32_t* src_row, int64_t M_cap, uint8_t* q, float* s, hipStream_t st) {
+  return sort_rows(xq, xs, T, H / 16, (int)(H / kTile), k, E, topk_idx, align, workspace, row_map, offsets, src_row,
+                   M_cap, q, s, st);
 }
 hipError_t launch_permute_fp8(const uint8_t* xq, const e8m0_t* xs, int64_t T, int64_t H, int k, int E,
-                              const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
-                              uint8_t* q, e8m0_t* s, hipStream_t st) {
-  return sort_rows(xq, xs, T, H / 16, (int)(H / kTile), k, E, row_map, offsets, src_row, M_cap, q, s, st);
+                              const int32_t* topk_idx, int align, void* workspace, int32_t* row_map, int32_t* offsets,
+                              int32_t* src_row, int64_t M_cap, uint8_t* q, e8m0_t* s, hipStream_t st) {
+  return sort_rows(xq, xs, T, H / 16, (int)(H / kTile), k, E, topk_idx, align, workspace, row_map, offsets, src_row,
+                   M_cap, q, s, st);
 }
 
 hipError_t launch_unpermute_bwd(const uint16_t* dy, const float* row_w, int64_t T, int64_t H, int k, int E,

@@ -505,8 +505,8 @@ def ff8_router_topk(logits, topk_idx, probs, bias=None, score="softmax", normali
     dev, st = _target(stream)
     _call(name, dev,
           _at(logits, dt, (T, E), "logits", dev), _at_n(bias, _f32, E, "bias", dev), T, E, k, SCORES[score],
-          int(bool(normalize)), scale, _at(topk_idx, _i32, (T, k), "topk_idx", dev), _at(probs, _f32, (T, k), "probs", dev),
-          st)
+          int(bool(normalize)), scale, _at(topk_idx, _i32, (T, k), "topk_idx", dev),
+          _at(probs, _f32, (T, k), "probs", dev), st)
 
 
 def ff8_router_topk_bwd(logits, topk_idx, dprobs, dlogits, score="softmax", normalize=False, scale=1.0, stream=None):
@@ -544,8 +544,8 @@ def ff8_permute_bf16(x, k, E, topk_idx, reuse_map, row_map, offsets, src_row, ou
     dev, st = _target(stream)
     idx, rm, off, src = _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row, dev)
     ws, n = _at_ws(workspace, dev)
-    _call("ff8_permute_bf16", dev, _at(x, _bf16, (T, H), "x", dev), T, H, k, E, idx, int(reuse_map), rm, off, src, M_cap,
-          _at(out, _bf16, (M_cap, H), "out", dev), ws, n, int(align), st)
+    _call("ff8_permute_bf16", dev, _at(x, _bf16, (T, H), "x", dev), T, H, k, E, idx, int(reuse_map), rm, off, src,
+          M_cap, _at(out, _bf16, (M_cap, H), "out", dev), ws, n, int(align), st)
 
 
 def ff8_permute_fp8(xq, xs, k, E, topk_idx, reuse_map, row_map, offsets, src_row, q, s, workspace=None, align=128,
@@ -559,8 +559,8 @@ def ff8_permute_fp8(xq, xs, k, E, topk_idx, reuse_map, row_map, offsets, src_row
     idx, rm, off, src = _maps(T, k, E, M_cap, topk_idx, row_map, offsets, src_row, dev)
     ws, n = _at_ws(workspace, dev)
     _call(name, dev,
-          _at(xq, _u8, (T, H), "xq", dev), _at(xs, sd, (T, H // 128), "xs", dev), T, H, k, E, idx, int(reuse_map), rm, off,
-          src, M_cap, _at(q, _u8, (M_cap, H), "q", dev), _at(s, sd, (M_cap, H // 128), "s", dev), ws, n, int(align), st)
+          _at(xq, _u8, (T, H), "xq", dev), _at(xs, sd, (T, H // 128), "xs", dev), T, H, k, E, idx, int(reuse_map), rm,
+          off, src, M_cap, _at(q, _u8, (M_cap, H), "q", dev), _at(s, sd, (M_cap, H // 128), "s", dev), ws, n, int(align), st)
 
 
 def ff8_unpermute_bwd(dy, row_w, k, E, row_map, offsets, src_row, dy_perm, y_perm=None, dprobs=None, stream=None):
@@ -572,8 +572,8 @@ def ff8_unpermute_bwd(dy, row_w, k, E, row_map, offsets, src_row, dy_perm, y_per
     _call("ff8_unpermute_bwd", dev,
           _at(dy, _bf16, (T, H), "dy", dev), _at_n(row_w, _f32, T * k, "row_w", dev), T, H, k, E, rm, off, src, M_cap,
           _at(dy_perm, _bf16, (M_cap, H), "dy_perm", dev),
-          None if y_perm is None else _at(y_perm, _bf16, (M_cap, H), "y_perm", dev), _at_n(dprobs, _f32, T * k, "dprobs", dev),
-          st)
+          None if y_perm is None else _at(y_perm, _bf16, (M_cap, H), "y_perm", dev),
+          _at_n(dprobs, _f32, T * k, "dprobs", dev), st)
 
 
 def ff8_quant_mxfp4(w, q, s, stream=None):
