@@ -516,10 +516,15 @@ hipError_t launch_grouped_gemv_mxfp4(const uint16_t* x, int64_t x_rows, const ui
     auto* const f = swiglu ? gemm_mxfp4_kernel<true> : gemm_mxfp4_kernel<false>;
     f<<<(unsigned)((blocks * nt + 7) / 8 * 8), kManyThreads, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, out);
   } else {
-    constexpr int kWaves = 4;
-    auto* const f = swiglu ? gemv_mxfp4_kernel<true, kWaves> : gemv_mxfp4_kernel<false, kWaves>;
-    f<<<(unsigned)(M_cap / 16 * (N / (16 * kTiles))), kWaves * 64, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row,
-                                                                            top_k, N, K, out);
+    // Two waves an item where K gives them at most six blocks each, otherwise four.  us, two waves / four: K = 1024,
+    // 32 experts, 8 and 32 tokens 8.4 / 9.8 and 9.8 / 11.3, 1408, 64 experts 13.2 / 14.1; 2048, one token 7.4 / 6.6, 32
+    // tokens 27.8 / 27.5; 7168, 16 tokens 80 / 76.  (With few blocks a wave has little to hide its start behind, and
+    // more workgroups fit beside one another; with many, two waves have too few loads in flight.)
+    const bool two = K <= 12 * kTile;
+    auto* const f = swiglu ? two ? gemv_mxfp4_kernel<true, 2> : gemv_mxfp4_kernel<true, 4>
+                           : two ? gemv_mxfp4_kernel<false, 2> : gemv_mxfp4_kernel<false, 4>;
+    f<<<(unsigned)(M_cap / 16 * (N / (16 * kTiles))), two ? 128 : 256, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row,
+                                                                                top_k, N, K, out);
   }
   return hipGetLastError();
 }
