@@ -164,19 +164,25 @@ __device__ __forceinline__ float packed_logit(uint32_t key) {
 // What a round has found, by slot of a group.
 struct Choice {
   int idx;
-  float logit, key;
+  float logit, key, bias;
 };
 template <int kSlots>
 struct Choices {
   int idx[kSlots];
-  float logit[kSlots], key[kSlots];
+  float logit[kSlots], key[kSlots], bias[kSlots];
   __device__ __forceinline__ void put(int i, const Choice& c) {
     idx[i] = c.idx;
     logit[i] = c.logit;
     key[i] = c.key;
+    bias[i] = c.bias;
   }
-  __device__ __forceinline__ Choice get(int i) const { return {idx[i], logit[i], key[i]}; }
+  __device__ __forceinline__ Choice get(int i) const { return {idx[i], logit[i], key[i], bias[i]}; }
 };
+// Whether the float32 keys of two experts tell their order: they are further apart than both may be off, or come
+// from equal logits and biases.
+__device__ __forceinline__ bool certain(const Choice& a, const Choice& b, float err) {
+  return (a.key - b.key > err + 0x1p-21f * fabsf(a.key)) | ((a.logit == b.logit) & (a.bias == b.bias));
+}
 
 // k rounds over keys of type K (-inf: never chosen): the largest of the group, the lowest lane that has it, its
 // lowest expert.  Slot j of `out` is written by the lane that held it; chosen keys become -inf.
@@ -209,17 +215,25 @@ __device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], 
       key[v] = hit ? (K)-INFINITY : key[v];
       mine = mine && !hit;
     }
-    if (lane == win) out.put(j, {top > -INFINITY ? lane * V + at : -1, logit, (float)top});
+    if (lane == win) out.put(j, {top > -INFINITY ? lane * V + at : -1, logit, (float)top, 0.0f});
   }
 }
 
-// The same by ranks, for 16 lanes and k <= 8, where that takes a fraction of the rounds' instructions: the k-th of
-// the lanes' largest keys bounds the k-th of all from below; the keys from there on (11 of 256 on average) go to
-// the lanes in expert order, one each (two each where a group of the wave has more than 16), and each lane counts
-// the better ones.  False, with nothing chosen, where there are more than 32.  Leaves the keys as they are.
+// The same by ranks, for 16 lanes (k <= 16), where that takes a fraction of the rounds' instructions: the k-th of the
+// lanes' largest keys bounds the k-th of all from below; the keys from there on (11 of 256 for k = 8, on average) go
+// to the lanes in expert order, one each (two where a group of the wave has more than 16), and each lane counts the
+// better ones.  With a bias the candidates begin as far below that as float32 may be off, and where the order
+// of two of them is not certain they are ranked again in float64: a few tokens in a thousand, and only these
+// experts (all 256 in float64 made such waves, and with them the launch, 8 us longer).
+// False, with nothing chosen, where there are more than 32.  Leaves the keys as they are.
 template <int N>
 __device__ __forceinline__ float from_left(float v) {  // of the lane N to the left, around the row
   return __uint_as_float(dpp<0x120 + N>(__float_as_uint(v)));
+}
+template <int N>
+__device__ __forceinline__ double from_left(double v) {
+  const u32x2 u = __builtin_bit_cast(u32x2, v);
+  return __builtin_bit_cast(double, u32x2{dpp<0x120 + N>(u[0]), dpp<0x120 + N>(u[1])});
 }
 template <int N>
 __device__ __forceinline__ int count_larger(float v, int n) {
@@ -228,14 +242,23 @@ __device__ __forceinline__ int count_larger(float v, int n) {
 }
 // Of the row's values `o`, how many come before this lane's v: larger, or equal and in a lane below `lane`
 // (kSelf: the lane's own `o` is another value, and counts as one in a lane below).
-template <int N, bool kSelf>
-__device__ __forceinline__ int count_before(float o, float v, int lane, int n) {
+template <int N, bool kSelf, typename K>
+__device__ __forceinline__ int count_before(K o, K v, int lane, int n) {
   if constexpr (N < 16) {
-    const float f = N == 0 ? o : from_left<N == 0 ? 1 : N>(o);
+    const K f = N == 0 ? o : from_left<N == 0 ? 1 : N>(o);
     if (N > 0 || kSelf) n += (f > v) | ((f == v) & (lane >= N));
     return count_before<N + 1, kSelf>(o, v, lane, n);
   }
   return n;
+}
+// Ranks of the lanes' first keys c and, with `two`, second keys d, in the order of the list c0 .. c15 d0 .. d15.
+template <typename K>
+__device__ __forceinline__ void ranks(K c, K d, bool two, int lane, int& rank_c, int& rank_d) {
+  rank_c = count_before<0, false>(c, c, lane, 0);
+  if (two) {
+    rank_c += count_before<0, true>(d, c, -1, 0);
+    rank_d = count_before<0, false>(d, d, lane, 0) + count_before<0, true>(c, d, 16, 0);
+  }
 }
 __device__ __forceinline__ int row_inclusive_sum(int v) {
   v += (int)dpp<0x111>((uint32_t)v);
@@ -244,48 +267,71 @@ __device__ __forceinline__ int row_inclusive_sum(int v) {
   v += (int)dpp<0x118>((uint32_t)v);
   return v;
 }
-template <int V, typename Out>
-__device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float (&l)[V], int k, Out& out) {
+// Score + bias in float64: sigmoid, or for softmax exp(l - m) / z with z the row's sum.
+template <bool kSigmoid>
+__device__ __forceinline__ double key64(float l, float b, float m, double z) {
+  const double s = kSigmoid ? 1.0 / (1.0 + exp(-(double)l)) : exp((double)l - (double)m) / z;
+  const double k = s + (double)b;
+  return ((l > -INFINITY) & (k > -INFINITY)) ? k : -INFINITY;
+}
+template <int L, int V, bool kSigmoid>
+__device__ __forceinline__ double row_sum64(const float (&l)[V], float m) {
+  double z = 0.0;
+  if (!kSigmoid) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) z += exp((double)l[v] - (double)m);
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) z += __shfl_xor(z, d);
+  }
+  return z;
+}
+template <int V, bool kSigmoid, bool kBias, typename Out>
+__device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float (&l)[V], const float* b, int k,
+                                              float err, float m, Out& out) {
   const int lane = threadIdx.x & 15;
   float best = key[0];
 #pragma unroll
   for (int v = 1; v < V; ++v) best = fmaxf(best, key[v]);
-  // at least the lowest finite number: a key of -inf is no candidate
-  const float bound = fmaxf(-group_max<16>(count_larger<1>(best, 0) < k ? -best : -INFINITY), -3.402823466e38f);
+  float bound = -group_max<16>(count_larger<1>(best, 0) < k ? -best : -INFINITY);
+  if (kBias) bound -= err + 0x1p-21f * fabsf(bound);
+  bound = fmaxf(bound, -3.402823466e38f);  // the lowest finite number: a key of -inf is no candidate
   int n = 0;
 #pragma unroll
   for (int v = 0; v < V; ++v) n += key[v] >= bound;
   const int end = row_inclusive_sum(n), total = (int)dpp<0x15F>((uint32_t)end);
   if (__any(total > 32)) return false;
+  const bool two = __any(total > 16);
   int at = end - n;
 #pragma unroll
   for (int v = 0; v < V; ++v)
-    if (key[v] >= bound) out.put(at++, {lane * V + v, l[v], key[v]});
+    if (key[v] >= bound) out.put(at++, {lane * V + v, l[v], key[v], kBias ? b[v] : 0.0f});
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  Choice c = {-1, -INFINITY, -INFINITY}, d = c;
+  Choice c = {-1, -INFINITY, -INFINITY, 0.0f}, d = c;
   if (lane < total) c = out.get(lane);
-  int rank = count_before<0, false>(c.key, c.key, lane, 0);
-  if (__any(total > 16)) {
-    if (lane + 16 < total) d = out.get(lane + 16);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    // every value of the first sixteen stands before an equal one of the second
-    rank += count_before<0, true>(d.key, c.key, -1, 0);
-    const int rank_d = count_before<0, false>(d.key, d.key, lane, 0) + count_before<0, true>(c.key, d.key, 16, 0);
-    if (rank_d < k) out.put(rank_d, d);
-  }
+  if (two && lane + 16 < total) d = out.get(lane + 16);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (rank < k) out.put(rank, c);
-  return true;
-}
-
-// True if the chosen keys are still there (the rounds leave -inf in their place).
-template <int L, int V, typename Out>
-__device__ __forceinline__ bool choose(float (&key)[V], const float (&l)[V], int k, Out& out) {
-  if constexpr (L == 16 && V > 1) {
-    if (k <= 8 && choose_ranked<V>(key, l, k, out)) return true;
+  int rank_c, rank_d = 32;
+  ranks(c.key, d.key, two, lane, rank_c, rank_d);
+  out.put(rank_c, c);  // (missing ones behind)
+  if (two) out.put(rank_d, d);
+  if (kBias) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // every two neighbours down to where the keys are clearly below the k-th
+    const float last = total >= k ? out.key[k - 1] : -INFINITY, near = last - (err + 0x1p-21f * fabsf(last));
+    bool unsure = false;
+    for (int r = lane; r + 1 < total; r += 16) {
+      const Choice x = out.get(r);
+      unsure |= !(x.key < near) & !certain(x, out.get(r + 1), err);
+    }
+    if (__any(unsure)) {
+      const double z = row_sum64<16, V, kSigmoid>(l, m);
+      ranks(key64<kSigmoid>(c.logit, c.bias, m, z), key64<kSigmoid>(d.logit, d.bias, m, z), two, lane, rank_c, rank_d);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      out.put(rank_c, c);
+      if (two) out.put(rank_d, d);
+    }
   }
-  choose_rounds<L, V>(key, l, k, out);
-  return false;
+  return true;
 }
 
 template <int L, int V, bool kSigmoid, bool kNormalize, bool kBias, typename X>
@@ -340,12 +386,12 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
     if (!kBias) {
 #pragma unroll
       for (int v = 0; v < V; ++v) key[v] = l[v] > -INFINITY ? l[v] : -INFINITY;  // NaN is never chosen
-      choose<L, V>(key, l, k, mine);
+      if (L != 16 || !choose_ranked<V, kSigmoid, false>(key, l, nullptr, k, 0.0f, 0.0f, mine))
+        choose_rounds<L, V>(key, l, k, mine);
     } else {
       // In float32 first.  Both scores are off by less than 2^-21 (sigmoid: the exponential's and the
       // reciprocal's unit, damped) or 2^-18 of the row's largest (softmax: a sum of up to 1024), the sum by
-      // half a unit.  A choice is certain where keys that it tells apart are further than twice that from one
-      // another, or come from equal logits and biases; any other row is decided in float64.
+      // half a unit; `err` is over twice that.  What float32 does not tell is decided in float64.
       const float inv = 1.0f / sum;
       float b[V];
       load_row<V>(bias, lane, E, vec_bias, 0.0f, b);
@@ -355,48 +401,30 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
         const float sum_b = s + b[v];
         key[v] = ((l[v] > -INFINITY) & (sum_b > -INFINITY)) ? sum_b : -INFINITY;
       }
-      const bool kept = choose<L, V>(key, l, k, mine);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       const float err = kSigmoid ? 0x1p-19f : 0x1p-16f * inv;
-      bool unsure = false;
-      if (lane + 1 < k) {
-        const Choice a = mine.get(lane), n = mine.get(lane + 1);
-        if (n.idx >= 0 && !(a.key - n.key > err + 0x1p-21f * fabsf(a.key)))
-          unsure = !(a.logit == n.logit && bias[a.idx] == bias[n.idx]);
-      }
-      const Choice last = mine.get(k - 1);
-      const float near = last.key - (err + 0x1p-21f * fabsf(last.key));
-      int n_near = 0;
+      if (L != 16 || !choose_ranked<V, kSigmoid, true>(key, l, b, k, err, m, mine)) {
+        choose_rounds<L, V>(key, l, k, mine);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        bool unsure = false;
+        auto of = [&](int j) {
+          Choice x = mine.get(j);
+          x.bias = x.idx >= 0 ? bias[x.idx] : 0.0f;
+          return x;
+        };
+        if (lane + 1 < k && mine.idx[lane + 1] >= 0) unsure = !certain(of(lane), of(lane + 1), err);
+        if (mine.idx[k - 1] >= 0) {  // the others (the rounds leave -inf in the place of a chosen key) below the last
+          const Choice last = of(k - 1);
 #pragma unroll
-      for (int v = 0; v < V; ++v) n_near += !(key[v] < near);
-      // beside the chosen
-      if (__any(last.idx >= 0 && group_sum<L>((float)n_near) > (kept ? (float)k : 0.0f))) {
-        const float lb = last.idx >= 0 ? bias[last.idx] : 0.0f;
-#pragma unroll
-        for (int v = 0; v < V; ++v)  // not chosen, not clearly below, and not equal in all
-          unsure |= (last.idx >= 0) & (key[v] > -INFINITY) & !(key[v] < near) &
-                    (!kept | (key[v] < last.key) | ((key[v] == last.key) & (lane * V + v > last.idx))) &
-                    !((l[v] == last.logit) & (b[v] == lb));
-      }
-      if (__any(unsure)) {
-        double z = 1.0, key64[V];
-        if (!kSigmoid) {
-          z = 0.0;
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            key64[v] = exp((double)l[v] - (double)m);
-            z += key64[v];
-          }
-#pragma unroll
-          for (int d = 1; d < L; d <<= 1) z += __shfl_xor(z, d);
+          for (int v = 0; v < V; ++v)
+            unsure |= (key[v] > -INFINITY) & !certain(last, {lane * V + v, l[v], key[v], b[v]}, err);
         }
+        if (__any(unsure)) {
+          const double z = row_sum64<L, V, kSigmoid>(l, m);
+          double wide[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const double s = kSigmoid ? 1.0 / (1.0 + exp(-(double)l[v])) : key64[v] / z;
-          const double sum_b = s + (double)b[v];
-          key64[v] = ((l[v] > -INFINITY) & (sum_b > -INFINITY)) ? sum_b : -INFINITY;  // a missing expert's l is -inf
+          for (int v = 0; v < V; ++v) wide[v] = key64<kSigmoid>(l[v], b[v], m, z);  // a missing expert's l is -inf
+          choose_rounds<L, V>(wide, l, k, mine);
         }
-        choose_rounds<L, V>(key64, l, k, mine);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

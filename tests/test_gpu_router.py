@@ -116,6 +116,24 @@ def test_ties_and_near_ties():
         _check(step, torch.full((E,), 8.0), 2, "softmax", False)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("T", [3, 2500])
+def test_order_that_float32_does_not_tell(score, T):
+    """Clusters of experts with equal logits and biases a few 2^-27 apart (one float32 step of the sums is 2^-24 and
+    more), some exactly equal: the order of every cluster, and where it ends the choice, is the float64 one."""
+    for E, n, k in ((16, 12, 8), (16, 16, 16), (48, 20, 8), (64, 30, 16), (256, 9, 8), (256, 24, 8), (256, 200, 8),
+                    (256, 40, 12), (600, 30, 20)):
+        rng = np.random.default_rng(E + n + k)
+        z = rng.normal(size=(T, E)).astype(np.float32) - 6.0
+        b = np.zeros(E, dtype=np.float32)
+        at = rng.permutation(E)[:n]
+        z[:, at] = 1.0
+        b[at] = rng.integers(0, n, size=n) * 2.0 ** -27  # duplicates among them
+        z[::3, at[: n // 3]] = 1.5                       # a second cluster in some rows
+        idx, _ = _run(torch.from_numpy(z), torch.from_numpy(b), k, score, True, 1.0)
+        assert np.array_equal(idx, router.choose(z, b, k, score)), (E, n, k)
+
+
 def test_scores_that_underflow():
     z = torch.full((2, 64), -200.0)
     z[0, 3], z[0, 9] = -150.0, -151.0
