@@ -12,10 +12,12 @@
 //   normalized, r_j     dl_j = c g_j r_j (dp_j - sum_m r_m dp_m),  g = 1 or sigmoid(-l_j)
 // and zero for experts that are not chosen in the last two.
 //
-// What bounds it.  The floor is one read of the logits (8.4 MB at 16384 tokens x 256 experts: about 1.5 us);
-// the work is k rounds of an argmax over the experts, so that is arranged to take few instructions: a token is
-// held by 16 lanes (or by a wave, for few tokens or many experts), its experts in registers, reductions run on
-// DPP and lane swaps instead of LDS, and bf16 logits carry their expert's number in the low half of one word.
+// What bounds it.  The floor is one read of the logits (8.4 MB at 16384 tokens x 256 experts: 1.4 us, of which
+// the choice is measured at 8.0 and the gradient, 17.8 MB and 2.7 us, at 7.0: a launch alone is about 2 and the
+// rest is instructions).  So those are kept few: a token is held by 16 lanes (or by a wave, for few tokens or many
+// experts), its experts in registers, reductions run on DPP and lane swaps instead of LDS, bf16 logits carry
+// their expert's number in the low half of one word for the k rounds of the maximum, and where they cannot, the
+// candidates for the k places are found and ranked by counting.
 
 #include <math.h>
 
@@ -538,16 +540,21 @@ __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict_
 }
 
 // Lanes a token.  Sixteen (four tokens a wave) take a quarter of the reductions of a whole wave but hold four
-// times the experts a lane: the wave is for few tokens, where a round's latency counts, for k above 16 (a
-// lane holds a slot) and for more than 256 experts.
-int lanes_of(int64_t T, int E, int k) {
+// times the experts a lane.  The wave is for k above 16 (a lane holds a slot), for more than 256 experts, and for
+// few tokens where the experts are chosen by rounds over packed keys or there are none to choose (`rounds`: bf16
+// logits without a bias, the gradient), as a round's latency counts there: 256 experts, k = 8, 16 against 64 lanes,
+// us: 1 token 3.4 2.1, 64 4.2 3.2, 2048 4.6 3.6, 4096 4.5 4.6, 16384 8.0 10.4; gradient 2.9 2.0, 3.4 3.1, 4.0 3.3,
+// 4.4 4.2, 7.0 9.2.  Up to 64 experts sixteen are as fast or faster from 64 tokens on (64: 2.5 2.9, 16384: 4.2 8.0),
+// and so they are at any number where 16 lanes choose by ranks (1 token 2.9 3.1 in float32, 3.6 3.9 with a bias;
+// 2048 tokens 4.7 5.0 and 5.5 8.7).
+int lanes_of(int64_t T, int E, int k, bool rounds) {
   if (E > 256 || k > 16) return 64;
-  return E > 64 && T <= 2048 ? 64 : 16;
+  return rounds && E > 64 && T <= 2048 ? 64 : 16;
 }
 
 // CALL(lanes, experts a lane)
-#define FF8_BY_SIZE(T, E, k, CALL)          \
-  if (lanes_of(T, E, k) == 16) {            \
+#define FF8_BY_SIZE(T, E, k, rounds, CALL)  \
+  if (lanes_of(T, E, k, rounds) == 16) {    \
     if ((E) <= 16) return CALL(16, 1);      \
     if ((E) <= 32) return CALL(16, 2);      \
     if ((E) <= 64) return CALL(16, 4);      \
@@ -615,7 +622,7 @@ hipError_t topk_impl(const X* logits, const float* bias, int64_t T, int E, int k
                      int32_t* idx, float* probs, hipStream_t st) {
   if (T == 0) return hipSuccess;
 #define FF8_CALL(L, V) topk_launch<L, V, X>(logits, bias, T, E, k, sig, norm, scale, idx, probs, st)
-  FF8_BY_SIZE(T, E, k, FF8_CALL)
+  FF8_BY_SIZE(T, E, k, sizeof(X) == 2 && !bias, FF8_CALL)
 #undef FF8_CALL
 }
 
@@ -624,7 +631,7 @@ hipError_t topk_bwd_impl(const X* logits, const int32_t* idx, const float* dprob
                          bool norm, float scale, X* dlogits, hipStream_t st) {
   if (T == 0) return hipSuccess;
 #define FF8_CALL(L, V) topk_bwd_launch<L, V, X>(logits, idx, dprobs, T, E, k, sig, norm, scale, dlogits, st)
-  FF8_BY_SIZE(T, E, k, FF8_CALL)
+  FF8_BY_SIZE(T, E, k, true, FF8_CALL)
 #undef FF8_CALL
 }
 
