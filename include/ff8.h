@@ -338,7 +338,7 @@ enum ff8_score {
  * ff8_router_topk -- the k experts of each token and their routing weights (the topk_idx and
  *   probs of ff8_permute_quant, ff8_unpermute and ff8_route) from the router's logits.
  *   logits   [T, E] float32.  -inf masks an expert; a NaN logit is never chosen (and makes the
- *            token's softmax weights NaN).
+ *            token's softmax weights NaN; with a bias and softmax scores that token chooses nothing).
  *   bias     [E] float32 or NULL.  Experts are chosen by the largest score + bias (in float64; an expert whose
  *            bias is -inf or NaN is never chosen), or, without a bias, by the largest logit; equal ones by the lower index.
  *            The bias does not enter the weights.
@@ -346,7 +346,7 @@ enum ff8_score {
  *   probs    [T, k] float32: scale * score, or with normalize = 1 scale * score / (sum of the chosen
  *            scores); 0 where topk_idx is -1.  Normalized weights stay exact where the scores
  *            themselves underflow.
- * Requires 1 <= k <= E <= 1024, k <= 64, score an ff8_score, normalize 0 or 1, scale finite, T * k < 2^31.
+ * Requires 1 <= k <= E <= 1024, k <= 64, score an ff8_score, normalize 0 or 1, scale finite, T <= 2^25.
  */
 int ff8_router_topk(const float* logits, const float* bias, int64_t T, int E, int k, int score, int normalize,
                     float scale, int32_t* topk_idx, float* probs, void* stream);
@@ -358,7 +358,7 @@ int ff8_router_topk_bf16(const ff8_bf16* logits, const float* bias, int64_t T, i
  * ff8_router_topk_bwd -- the gradient of the logits through the routing weights (the choice itself has
  *   none, nor has the bias): dlogits [T, E] from dprobs [T, k] float32, the logits and the forward's
  *   topk_idx.  Every element of dlogits is written.  Slots of -1 add nothing, whatever dprobs holds
- *   there.  score, normalize and scale as in the forward.  dlogits has the logits' type.
+ *   there.  score, normalize and scale as in the forward.  dlogits has the logits' type and is apart from them.
  */
 int ff8_router_topk_bwd(const float* logits, const int32_t* topk_idx, const float* dprobs, int64_t T, int E, int k,
                         int score, int normalize, float scale, float* dlogits, void* stream);
@@ -376,7 +376,7 @@ int ff8_route(const int32_t* topk_idx, int64_t T, int k, int E, int32_t* row_map
  * ff8_permute_bf16 -- ff8_permute_quant_aligned without the cast: out[row_map[t, j]] = x[t], padding rows
  *   zero, rows >= offsets[E] untouched.  Its gradient is ff8_unpermute without weights.
  *   x [T, H] bf16; out [M_cap, H] bf16; x and out 16-byte aligned and apart from one another.  Maps,
- *   reuse_map, workspace and requirements as there.
+ *   reuse_map, workspace and requirements as there; T * k <= 2^25.
  */
 int ff8_permute_bf16(const ff8_bf16* x, int64_t T, int64_t H, int k, int E, const int32_t* topk_idx, int reuse_map,
                      int32_t* row_map, int32_t* offsets, int32_t* src_row, int64_t M_cap, ff8_bf16* out,
@@ -403,7 +403,7 @@ int ff8_permute_fp8_e8m0(const ff8_e4m3* xq, const ff8_e8m0* xs, int64_t T, int6
  *     dprobs[t, j] = sum_h dy[t, h] * y_perm[row_map[t, j], h] in float32, 0 for a dropped slot.
  *   dy [T, H] bf16; row_w, dprobs [T, k] float32; row_map, offsets, src_row as the forward's; y_perm, dy_perm
  *   [M_cap, H] bf16 (16-byte aligned; rows >= offsets[E] neither read nor written).  y_perm and dprobs may
- *   both be NULL: dy_perm alone.  Requires k <= 64.
+ *   both be NULL: dy_perm alone.  Requires k <= 64 and T * k <= 2^25.
  */
 int ff8_unpermute_bwd(const ff8_bf16* dy, const float* row_w, int64_t T, int64_t H, int k, int E,
                       const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
@@ -417,7 +417,7 @@ int ff8_unpermute_bwd(const ff8_bf16* dy, const float* row_w, int64_t T, int64_t
  *   w [rows, cols] bf16, finite; q [rows, cols/2]; s [rows, cols/32].
  *   A group's T is the smallest integer >= -126 with max|w| <= 6 * 2^T (no value saturates; an all-zero group
  *   gets -126), the rule of the e4m3 scales; codes are rounded to nearest, ties to even, sign kept.
- *   rows >= 1, cols a multiple of 128, rows * cols < 2^35.
+ *   rows >= 1, cols a multiple of 128, rows * cols < 2^34.
  */
 int ff8_quant_mxfp4(const ff8_bf16* w, int64_t rows, int64_t cols, uint8_t* q, ff8_e8m0* s, void* stream);
 
@@ -439,13 +439,14 @@ int ff8_pack_mxfp4(const uint8_t* q, const ff8_e8m0* s, int64_t rows, int64_t co
  *   bf16 activations, float32 sums, rounded once to bf16.
  *   tq, ts   the weights [E, N, K] as ff8_pack_mxfp4 lays them out.  Every code * 2^T must be finite in bf16
  *            (a scale byte of 255 is NaN).
+ *   offsets  [E + 1], from ff8_route or a permute: groups of multiples of 16 rows, offsets[E] <= M_cap.
  *   src_row  [M_cap] or NULL (every row below offsets[E] holds data).  With it, rows whose entry is -1 are
  *            padding: nothing of x is read for them, and out gets zeros.
  *   top_k    0: x [x_rows = M_cap, K] holds the grouped rows.  k >= 1: x [x_rows = T, K] holds the tokens, and row m
  *            takes token src_row[m] / top_k (src_row required): no permute is needed in front.
  *   out      [M_cap, N] bf16; rows >= offsets[E] untouched.
  *   E <= 1024; M_cap, N, K multiples of 128; x_rows and M_cap below 2^31, x_rows * K below 2^35, M_cap * N below
- *   2^41; x, tq, ts and out 16-byte aligned.
+ *   2^34; x, tq, ts and out 16-byte aligned.
  */
 int ff8_grouped_gemv_mxfp4(const ff8_bf16* x, int64_t x_rows, const uint8_t* tq, const ff8_e8m0* ts,
                            const int32_t* offsets, int E, const int32_t* src_row, int top_k, int64_t M_cap, int64_t N,

@@ -368,14 +368,20 @@ int ff8_unpermute(const ff8_bf16* y_perm, const int32_t* row_map, const float* r
 
 }  // extern "C"
 
+// Tokens of a router call and (token, slot) pairs of a row sort: a wave each at the most, and a launch has fewer
+// than 2^32 threads.
+static constexpr int64_t kMaxRows = (int64_t)1 << 25;
+static int pairs_validate(const char* fn, int64_t T, int k) {
+  return T <= kMaxRows / k ? FF8_OK : fail(FF8_ERR_SHAPE, "%s: T * k must be at most 2^25", fn);
+}
+
 static int router_validate(const char* fn, const void* logits, int64_t T, int E, int k, int score, int normalize,
                            float scale, const void* topk_idx, const void* weights, const void* out) {
   if (!(k >= 1 && k <= E && E <= 1024 && k <= 64)) return fail(FF8_ERR_ARG, "%s: need 1 <= k <= E <= 1024, k <= 64", fn);
   if (score != FF8_SCORE_SOFTMAX && score != FF8_SCORE_SIGMOID) return fail(FF8_ERR_ARG, "%s: unknown score", fn);
   if (!(normalize == 0 || normalize == 1)) return fail(FF8_ERR_ARG, "%s: normalize must be 0 or 1", fn);
   if (!std::isfinite(scale)) return fail(FF8_ERR_ARG, "%s: scale must be finite", fn);
-  if (!(T >= 0 && T < ((int64_t)1 << 31) && T * k < ((int64_t)1 << 31)))
-    return fail(FF8_ERR_SHAPE, "%s: need T >= 0 and T * k < 2^31", fn);
+  if (!(T >= 0 && T <= kMaxRows)) return fail(FF8_ERR_SHAPE, "%s: need 0 <= T <= 2^25", fn);
   if (T > 0 && (!logits || !topk_idx || !weights || !out)) return fail(FF8_ERR_NULL, "%s: a tensor is NULL", fn);
   return FF8_OK;
 }
@@ -434,6 +440,7 @@ int ff8_permute_bf16(const ff8_bf16* x, int64_t T, int64_t H, int k, int E, cons
   const int rc = permute_validate(__func__, x, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, out,
                                   out, workspace, ws_bytes, align, true);
   if (rc != FF8_OK) return rc;
+  if (pairs_validate(__func__, T, k) != FF8_OK) return FF8_ERR_SHAPE;
   REQUIRE_ALIGNED(x); REQUIRE_ALIGNED(out);
   return hip_status(ff8::launch_permute_bf16(x, T, H, k, E, reuse_map ? nullptr : topk_idx, align, workspace, row_map,
                                              offsets, src_row, M_cap, out, as_stream(stream)),
@@ -449,6 +456,7 @@ static int permute_fp8(const char* fn, const ff8_e4m3* xq, const SC* xs, int64_t
   const int rc = permute_validate(fn, xq, T, H, k, E, topk_idx, reuse_map, row_map, offsets, src_row, M_cap, q, s,
                                   workspace, ws_bytes, align, true);
   if (rc != FF8_OK) return rc;
+  if (pairs_validate(fn, T, k) != FF8_OK) return FF8_ERR_SHAPE;
   if (T > 0 && !xs) return fail(FF8_ERR_NULL, "%s: xs is NULL", fn);
   if ((reinterpret_cast<uintptr_t>(xq) | reinterpret_cast<uintptr_t>(q)) % 16 != 0)
     return fail(FF8_ERR_ARG, "%s: xq and q must be 16-byte aligned", fn);
@@ -467,8 +475,9 @@ static int gemv_mxfp4(const char* fn, const ff8_bf16* x, int64_t x_rows, const u
     return fail(FF8_ERR_SHAPE, "%s: M_cap, the weights' rows and K must be multiples of 128", fn);
   if (!(M_cap < ((int64_t)1 << 31) && x_rows >= 0 && x_rows < ((int64_t)1 << 31)))
     return fail(FF8_ERR_SHAPE, "%s: M_cap and x_rows must be below 2^31", fn);
-  if (!(x_rows < ((int64_t)1 << 35) / K && M_cap / 16 < ((int64_t)1 << 31) / (N / 64)))
-    return fail(FF8_ERR_SHAPE, "%s: x_rows * K must be below 2^35 and M_cap * N below 2^41", fn);
+  // one launch: 256 threads for 16 rows and 64 weight rows
+  if (!(x_rows < ((int64_t)1 << 35) / K && M_cap / 16 < ((int64_t)1 << 24) / (N / 64)))
+    return fail(FF8_ERR_SHAPE, "%s: x_rows * K must be below 2^35 and M_cap * N below 2^34", fn);
   if (top_k == 0 && x_rows != M_cap) return fail(FF8_ERR_SHAPE, "%s: grouped rows: x_rows must be M_cap", fn);
   if ((x_rows > 0 && !x) || !tq || !ts || !offsets || !out) return fail(FF8_ERR_NULL, "%s: a tensor is NULL", fn);
   if (top_k > 0 && !src_row) return fail(FF8_ERR_NULL, "%s: src_row is NULL", fn);
@@ -503,6 +512,7 @@ int ff8_unpermute_bwd(const ff8_bf16* dy, const float* row_w, int64_t T, int64_t
   const int rc = permute_validate(__func__, dy, T, H, k, E, nullptr, 1, row_map, offsets, src_row, M_cap, dy_perm,
                                   dy_perm, nullptr, 0, 16, true);
   if (rc != FF8_OK) return rc;
+  if (pairs_validate(__func__, T, k) != FF8_OK) return FF8_ERR_SHAPE;
   REQUIRE_ARG(k <= 64);
   if (T > 0) {
     REQUIRE_PTR(row_w);
@@ -519,7 +529,7 @@ int ff8_unpermute_bwd(const ff8_bf16* dy, const float* row_w, int64_t T, int64_t
 
 int ff8_quant_mxfp4(const ff8_bf16* w, int64_t rows, int64_t cols, uint8_t* q, ff8_e8m0* s, void* stream) {
   REQUIRE_PTR(w); REQUIRE_PTR(q); REQUIRE_PTR(s);
-  REQUIRE_SHAPE(rows >= 1 && mult128(cols) && rows < ((int64_t)1 << 35) / cols);
+  REQUIRE_SHAPE(rows >= 1 && mult128(cols) && rows < ((int64_t)1 << 34) / cols);
   REQUIRE_ALIGNED(w); REQUIRE_ALIGNED(q);
   return hip_status(ff8::launch_quant_mxfp4(w, rows, cols, q, s, as_stream(stream)), __func__);
 }

@@ -151,3 +151,17 @@ def test_binding_checks_shapes_and_types():
     # consistent calls stop at the device check here
     with pytest.raises(ValueError, match="device tensor"):
         ff8.ff8_grouped_gemv_mxfp4(e(M, K), tq, ts, off, e(M, N))
+
+
+def test_sizes_of_one_launch(lib):
+    """Beyond these a launch would have 2^32 threads or more."""
+    big = 1 << 25
+    assert lib.ff8_router_topk_bf16(P, None, big + 1, 8, 1, 0, 0, 1.0, P, P, None) == SHAPE
+    assert lib.ff8_router_topk_bwd(P, P, P, big + 1, 8, 1, 0, 0, 1.0, P, None) == SHAPE
+    M = 1 << 27
+    assert lib.ff8_permute_bf16(P, big, 128, 2, 4, P, 0, P, P, P, M, P, P, 1 << 40, 16, None) == SHAPE
+    assert lib.ff8_permute_fp8(P, P, big, 128, 2, 4, P, 0, P, P, P, M, P, P, P, 1 << 40, 16, None) == SHAPE
+    assert lib.ff8_unpermute_bwd(P, P, big, 128, 2, 4, P, P, P, M, P, P, P, None) == SHAPE
+    assert b"2^25" in lib.ff8_last_error()
+    assert lib.ff8_quant_mxfp4(P, 1 << 27, 128, P, P, None) == SHAPE
+    assert lib.ff8_grouped_gemv_mxfp4(P, 4, P, P, P, 4, P, 1, 1 << 21, 1 << 13, 128, P, None) == SHAPE
