@@ -7,8 +7,9 @@
 // are float32.  With few rows the weights are the traffic, so they are stored in the order in which
 // the matrix instruction takes them (ff8_pack_mxfp4): a tile of 16 rows x 128 columns is 1 KiB in
 // which lane l's 16 bytes are row l % 16, columns 32 (l / 16) .. + 31 -- one scale group -- and a
-// wave's load is contiguous; a lane's scales of the two tiles of 32 rows stand side by side.  From row-major weights the same kernel reached 3.4 TB/s, from tiles 6.1
-// (8 experts, 4096 x 7168, one row each): a wave's 16-byte loads then fall in 16 rows.
+// wave's load is contiguous; a lane's scales of the two tiles of 32 rows stand side by side.  From row-major weights
+// the same kernel reached 3.4 TB/s, from tiles 6.1 (8 experts, 4096 x 7168, one row each): a wave's 16-byte loads
+// of row-major weights fall in 16 rows.
 
 #include <math.h>
 
@@ -149,8 +150,16 @@ __device__ __forceinline__ int x_place(int r, int p) { return r * 16 + (p ^ ((r 
 // expert has to be looked up.  A wave brings its own piece of x through LDS into the order of the matrix
 // instruction; in registers it has two blocks of weights and x in flight.
 //
+// Bound by the weights' bytes.  One token of 7168 columns, 8 experts of 2 x 2048 rows with SwiGLU (125 MB): 21.0 us,
+// 5.9 TB/s, where a read of that size out of HBM takes 18.1; 7 tokens of 6 among 64 experts, 2048 x 1408 (49 MB): 11.4
+// us, 7.1 at the same rate, the rest being the launch and the first block of each wave.  Of the two blocks ahead:
+// three or more spill, and loads repeated behind a wave's last block, for a loop without its tail, cost 5 to 15%.
+//
 // The products of a wave's blocks, into its part of LDS.  kX: 16-byte pieces of x that a lane brings for a block,
 // four rows each; with one only the first four rows are there (the other columns of the products are not stored).
+// One where the block has no row of data behind its fourth, four otherwise.  us, one / always four: 1 token, 32
+// experts, k = 8, 7168 x 2048 up 22.0 / 22.4, down 14.3 / 15.0; 4 tokens up 55.2 / 57.4; 7 tokens, 64 experts, k = 6,
+// 2048 x 1408 up 21.0 / 22.0, down 11.4 / 12.1.
 template <bool kSwiglu, int kWaves, int kX>
 __device__ __forceinline__ void few_rows(const uint16_t* __restrict__ x, int src, unsigned mask,
                                          const Weights<kSwiglu>& w, int wave, int64_t K, float* part) {
@@ -281,6 +290,13 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
 // A workgroup of four waves computes 256 weight rows (64 a wave) for up to 96 token rows of one expert: every
 // wave goes through all column blocks and shares the block of x, which the workgroup brings into one of two LDS
 // buffers while it computes from the other.
+//
+// Bound by the matrix cores and the loads together: 32 experts with 32 rows on average, 7168 columns, 2 x 2048 rows
+// (511 MB): 131 to 138 us, 3.8 TB/s.  The loads alone take 94 us (74 at the rate of a large read), the matrix
+// instructions alone 101 (61 at that of a large product, 1370 TFLOP/s): experts' rows come in 16s, and one
+// CU's are not another's.  Together they draw the clock from 2.45 to 1.97 GHz, so that the sum of cycles stays
+// near the larger of the two and the time does not.  Blocks of 48 or 64 rows and weights three blocks
+// ahead were slower.
 constexpr int kManyWaves = 4, kManyThreads = 64 * kManyWaves, kManyRows = 96;
 
 // Workgroup b of a launch runs on XCD b % 8.  Each XCD takes an eighth of the (row block, weight rows) items, in
@@ -330,7 +346,9 @@ __device__ __forceinline__ RowBlock find_block(unsigned nt, const int32_t* __res
   return {-1, 0, 0, 0};
 }
 
-// The products of one workgroup with kM x 16 token rows.
+// The products of one workgroup with kM x 16 token rows: as many 16s as the block has rows of data.  us, so / always
+// six: 128 tokens of 2 among 8 experts, 4096 x 7168 up 57 / 88; 128 of 8 among 64, 2048 x 1408 down 25 / 43; the case
+// above 138 / 160.
 template <bool kSwiglu, int kM>
 __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const int* __restrict__ rows,
                                           const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts, int e,
@@ -436,7 +454,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void gemm_mxfp4_kernel(
     const int32_t* __restrict__ offsets, int E, const int32_t* __restrict__ src_row, int top_k, int64_t M_cap,
     int64_t N, int64_t K, uint16_t* __restrict__ out) {
   __shared__ u32x4 xs[2 * kManyRows * 16];
-  __shared__ int rows[kManyRows];
+  __shared__ int rows[128];  // two a lane of the first wave; the first kManyRows are used
   constexpr int kCols = kSwiglu ? kTiles * 8 : kTiles * 16;  // of out, a wave
   const int64_t n_out = kSwiglu ? N / 2 : N;
   const unsigned nt = (unsigned)((n_out + kManyWaves * kCols - 1) / (kManyWaves * kCols));

@@ -106,7 +106,8 @@ __global__ __launch_bounds__(kThreads) void sort_rows_kernel(const u32x4* __rest
 // knows the group offsets and its rows.  Behind those, one workgroup an expert fills the group's padding.  Integer
 // LDS atomics: the counts do not depend on order.  Against the routing in launches of its own (us): 1024 tokens x
 // 256 columns, 8 experts, k = 2 6.9 / 11.4; 512 x 7168, 64 experts, k = 8 17 / 26, with 128-row padding 29 / 38; 4096 x
-// 256, 1024 experts, k = 1 10.4 / 12.7.
+// 256, 1024 experts, k = 1 10.4 / 12.7.  Twice as many pairs are where it turns: 8192 x 256, 8 experts, k = 1 14.8 / 12.6,
+// 1024 x 2048, 64 experts, k = 8 14.9 / 17.7; and four times as many 36 / 13 and 30 / 24.
 constexpr int kMaxExperts = 1024, kMaxPairs = 4096;
 template <typename S>
 __global__ __launch_bounds__(kThreads) void route_sort_kernel(const u32x4* __restrict__ x, const S* __restrict__ s,
