@@ -101,32 +101,75 @@ __global__ __launch_bounds__(kThreads) void sort_rows_kernel(const u32x4* __rest
   if (r >= 0 && r < M_cap) move_row<S>(x, s, t, r, lane, row16, n_s, out, s_out);
 }
 
-// Routing and rows in one launch, for routings that every workgroup can count by itself (T * k <= 4096): a
-// workgroup takes eight (token, slot) pairs, counts all the pairs of each expert and those before its own, and so
-// knows the group offsets and its rows.  Behind those, one workgroup an expert fills the group's padding.  Integer
-// LDS atomics: the counts do not depend on order.  Against the routing in launches of its own (us): 1024 tokens x
-// 256 columns, 8 experts, k = 2 6.9 / 11.4; 512 x 7168, 64 experts, k = 8 17 / 26, with 128-row padding 29 / 38; 4096 x
-// 256, 1024 experts, k = 1 10.4 / 12.7.  Twice as many pairs are where it turns: 8192 x 256, 8 experts, k = 1 14.8 / 12.6,
-// 1024 x 2048, 64 experts, k = 8 14.9 / 17.7; and four times as many 36 / 13 and 30 / 24.
+// Routing and rows in one launch: a workgroup takes kWaves * kPer (token, slot) pairs, finds the pairs of each
+// expert and those before its own, and so knows the group offsets and its rows.  Behind those, one workgroup an
+// expert fills the group's padding.  Integer LDS atomics: the counts do not depend on order.
+// Up to kMaxPairs pairs every workgroup counts them all by itself.  us, so / with the routing in launches of its own:
+// 1024 tokens x 256 columns, 8 experts, k = 2 6.9 / 11.4; 512 x 7168, 64 experts, k = 8 17 / 26, with 128-row padding
+// 29 / 38; 4096 x 256, 1024 experts, k = 1 10.4 / 12.7.  (8192 x 256, 8 experts, k = 1 14.8 / 12.6.)
+// Otherwise a launch in front has counted chunks of kChunk tokens, and a workgroup adds those up and counts in its own
+// chunk alone; it then takes two pairs a wave: 16384 x 2048, 64 experts, k = 16 one, two, four, eight 236 215 215 216,
+// 8192 x 256, 8 experts, k = 1 11.1 9.8 10.0 12.5, 4096 x 7168, 256 experts, k = 8 149 143 144 143 us.
 constexpr int kMaxExperts = 1024, kMaxPairs = 4096;
-template <typename S>
-__global__ __launch_bounds__(kThreads) void route_sort_kernel(const u32x4* __restrict__ x, const S* __restrict__ s,
-                                                              const int32_t* __restrict__ topk_idx, int n_pairs, int k,
-                                                              int E, int align, int64_t row16, int n_s, int64_t M_cap,
-                                                              int32_t* __restrict__ row_map,
-                                                              int32_t* __restrict__ offsets,
-                                                              int32_t* __restrict__ src_row, u32x4* __restrict__ out,
-                                                              S* __restrict__ s_out) {
-  __shared__ unsigned count[kMaxExperts];  // pairs of an expert, and those before the workgroup's in the high half
-  __shared__ int start[kMaxExperts + 1], wave_sum[kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n_sort = (n_pairs + kWaves - 1) / kWaves, pad = (int)blockIdx.x - n_sort;  // pad: the expert, or below 0
-  const int p0 = (int)blockIdx.x * kWaves;
-  for (int e = tid; e < E; e += kThreads) count[e] = 0;
+constexpr int kChunk = kRouteChunk, kPerCounted = 2;
+__global__ __launch_bounds__(kThreads) void chunk_count_kernel(const int32_t* __restrict__ topk_idx, int n_pairs, int k,
+                                                               int E, int32_t* __restrict__ counts) {
+  __shared__ int count[kMaxExperts];
+  for (int e = threadIdx.x; e < E; e += kThreads) count[e] = 0;
   __syncthreads();
-  for (int i = tid; i < n_pairs; i += kThreads) {
+  const int p0 = (int)blockIdx.x * kChunk * k, p1 = p0 + kChunk * k < n_pairs ? p0 + kChunk * k : n_pairs;
+  for (int i = p0 + (int)threadIdx.x; i < p1; i += kThreads) {
     const int e = topk_idx[i];
-    if (e >= 0 && e < E) atomicAdd(&count[e], i < p0 ? 0x10001u : 1u);
+    if (e >= 0 && e < E) atomicAdd(&count[e], 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += kThreads) counts[(int)blockIdx.x * E + e] = count[e];
+}
+
+template <typename S, int kPer>
+__global__ __launch_bounds__(kThreads) void route_sort_kernel(
+    const u32x4* __restrict__ x, const S* __restrict__ s, const int32_t* __restrict__ topk_idx, int n_pairs, int k, int E,
+    int align, const int32_t* __restrict__ counts, int n_chunks, int64_t row16, int n_s, int64_t M_cap,
+    int32_t* __restrict__ row_map, int32_t* __restrict__ offsets, int32_t* __restrict__ src_row,
+    u32x4* __restrict__ out, S* __restrict__ s_out) {
+  __shared__ int total[kMaxExperts], before[kMaxExperts];  // pairs of an expert, and those before the workgroup's
+  __shared__ int start[kMaxExperts + 1], wave_sum[kWaves];
+  constexpr int kBlock = kWaves * kPer;
+  static_assert(kBlock <= 64, "a lane holds a pair");
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n_sort = (n_pairs + kBlock - 1) / kBlock, pad = (int)blockIdx.x - n_sort;  // pad: the expert, or below 0
+  const int p0 = pad < 0 ? (int)blockIdx.x * kBlock : 0;
+  const int mine = lane < kBlock && p0 + lane < n_pairs ? topk_idx[p0 + lane] : -1;
+  for (int e = tid; e < E; e += kThreads) {
+    total[e] = 0;
+    before[e] = 0;
+  }
+  __syncthreads();
+  int from = 0;  // the first pair that is not counted in `before` yet
+  if (counts) {
+    const int chunk = p0 / (kChunk * k);
+    from = chunk * kChunk * k;
+    // a thread adds up one expert's counts, of every stride-th chunk
+    const int stride = E < kThreads ? kThreads / E : 1;
+    for (int e0 = 0; e0 < E; e0 += kThreads) {
+      const int e = e0 + (E < kThreads ? tid % E : tid);
+      int all = 0, front = 0;
+      if (e < E)
+        for (int c = E < kThreads ? tid / E : 0; c < (tid / E < stride ? n_chunks : 0); c += stride) {
+          const int n = counts[c * E + e];
+          all += n;
+          front += c < chunk ? n : 0;
+        }
+      if (all) atomicAdd(&total[e], all);
+      if (front) atomicAdd(&before[e], front);
+    }
+  }
+  for (int i = from + tid; i < (counts ? p0 : n_pairs); i += kThreads) {
+    const int e = topk_idx[i];
+    if (e >= 0 && e < E) {
+      if (!counts) atomicAdd(&total[e], 1);
+      if (i < p0) atomicAdd(&before[e], 1);
+    }
   }
   __syncthreads();
   // group offsets: two experts a thread, scanned over the wave and the waves
@@ -134,7 +177,7 @@ __global__ __launch_bounds__(kThreads) void route_sort_kernel(const u32x4* __res
   int rows[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int e = 2 * tid + h, n = e < E ? (int)(count[e] & 0xFFFFu) : 0;
+    const int e = 2 * tid + h, n = e < E ? total[e] : 0;
     rows[h] = (n + align - 1) / align * align;
   }
   int end = rows[0] + rows[1];
@@ -153,25 +196,25 @@ __global__ __launch_bounds__(kThreads) void route_sort_kernel(const u32x4* __res
   if (blockIdx.x == 0)
     for (int e = tid; e <= E; e += kThreads) offsets[e] = start[e];
   if (pad < 0) {
-    const int p = __builtin_amdgcn_readfirstlane(p0 + wave);
-    if (p >= n_pairs) return;
-    const int mine = p0 + lane < n_pairs && lane < kWaves ? topk_idx[p0 + lane] : -1;
-    const int e = __builtin_amdgcn_readlane(mine, wave);
-    if (e < 0 || e >= E) {
-      if (lane == 0) row_map[p] = -1;
-      return;
+    for (int i = 0; i < kPer; ++i) {
+      const int slot = __builtin_amdgcn_readfirstlane(wave) + i * kWaves, p = p0 + slot;
+      if (p >= n_pairs) return;
+      const int e = __builtin_amdgcn_readlane(mine, slot);
+      if (e < 0 || e >= E) {
+        if (lane == 0) row_map[p] = -1;
+        continue;
+      }
+      const int64_t r = start[e] + before[e] + __popcll(__ballot(mine == e && lane < slot));
+      if (r >= M_cap) continue;
+      if (lane == 0) {
+        row_map[p] = (int)r;
+        src_row[r] = p;
+      }
+      move_row<S>(x, s, p / k, r, lane, row16, n_s, out, s_out);
     }
-    const unsigned long long before = __ballot(mine == e && lane < wave);
-    const int64_t r = start[e] + (int)(count[e] >> 16) + __popcll(before);
-    if (r >= M_cap) return;
-    if (lane == 0) {
-      row_map[p] = (int)r;
-      src_row[r] = p;
-    }
-    move_row<S>(x, s, p / k, r, lane, row16, n_s, out, s_out);
   } else {
     const int64_t r1 = start[pad + 1] < M_cap ? start[pad + 1] : M_cap;
-    for (int64_t r = start[pad] + (int)(count[pad] & 0xFFFFu) + wave; r < r1; r += kWaves) {
+    for (int64_t r = start[pad] + total[pad] + wave; r < r1; r += kWaves) {
       if (lane == 0) src_row[r] = -1;
       clear_row<S>(r, lane, row16, n_s, out, s_out);
     }
@@ -226,6 +269,15 @@ __global__ __launch_bounds__(kThreads) void return_bwd_kernel(
   }
 }
 
+// Whether routing and rows share a launch behind chunk counts (otherwise the routing has its own launches).  Every
+// workgroup of 16 pairs reads the counts and half a chunk, which pays while the workgroups are few and their rows long.
+// us, with / without: 100 tokens x 256 columns, 64 experts, k = 64 12 / 42; 1024 x 2048, 64, k = 8 12.5 / 18.5; 4096 x
+// 7168, 256, k = 8 143 / 153; 5001 x 7168 bytes, 32, k = 8 60 / 64.  Beyond: 32000 x 256, 8, k = 2 31 / 23; 8192 x 7168, 32, k
+// = 8 211 / 207, 16384 tokens 427 / 409; 16384 x 256, 64, k = 4 (4096 counts) 36 / 27.
+bool counted(int64_t n_pairs, int64_t n_counts, int64_t row16) {
+  return n_pairs <= (row16 >= 256 ? 48 << 10 : 32 << 10) && n_pairs * n_counts <= (int64_t)1 << 27;
+}
+
 unsigned grid_of(int64_t n_pairs, int E) { return (unsigned)(E + (n_pairs + kWaves - 1) / kWaves); }
 
 // With topk_idx the routing maps are built too.
@@ -237,11 +289,22 @@ hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_
   u32x4* const to = static_cast<u32x4*>(out);
   const int64_t n_pairs = T * k;
   if (topk_idx || T == 0) {
+    const int64_t n_chunks = (T + kChunk - 1) / kChunk;
+    int32_t* const counts = static_cast<int32_t*>(workspace);
+#define FF8_GO(PER, COUNTS)                                                                                         \
+  route_sort_kernel<S, PER><<<(unsigned)(E + (n_pairs + kWaves * PER - 1) / (kWaves * PER)), kThreads, 0, st>>>(    \
+      in, s, topk_idx, (int)n_pairs, k, E, align, COUNTS, (int)n_chunks, row16, n_s, M_cap, row_map, offsets, \
+      src_row, to, s_out)
     if (n_pairs <= kMaxPairs) {
-      route_sort_kernel<S><<<grid_of(n_pairs, E), kThreads, 0, st>>>(in, s, topk_idx, (int)n_pairs, k, E, align, row16,
-                                                                     n_s, M_cap, row_map, offsets, src_row, to, s_out);
+      FF8_GO(1, nullptr);
       return hipGetLastError();
     }
+    if (counted(n_pairs, n_chunks * E, row16)) {
+      chunk_count_kernel<<<(unsigned)n_chunks, kThreads, 0, st>>>(topk_idx, (int)n_pairs, k, E, counts);
+      FF8_GO(kPerCounted, counts);
+      return hipGetLastError();
+    }
+#undef FF8_GO
     const hipError_t e = launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace, st);
     if (e != hipSuccess) return e;
   }

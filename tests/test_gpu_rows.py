@@ -14,7 +14,10 @@ pytestmark = pytest.mark.gpu
 # T, H, E, k, align, fraction of dropped slots
 CASES = [(1, 128, 1, 1, 128, 0.0), (1, 256, 8, 8, 16, 0.0), (7, 2048, 64, 6, 16, 0.1), (300, 384, 6, 2, 32, 0.5),
          (517, 1408, 64, 6, 16, 0.05), (1024, 256, 8, 2, 128, 0.0), (257, 128, 1024, 3, 64, 0.0),
-         (64, 16384, 2, 2, 128, 0.0), (60, 8320, 5, 5, 16, 0.3), (130, 256, 64, 64, 16, 0.1), (5, 128, 4, 2, 16, 1.0)]
+         (64, 16384, 2, 2, 128, 0.0), (60, 8320, 5, 5, 16, 0.3), (130, 256, 64, 64, 16, 0.1), (5, 128, 4, 2, 16, 1.0),
+         # routing by chunks of 256 tokens, in the rows' launch and in launches of its own
+         (700, 256, 40, 7, 16, 0.1), (3000, 128, 24, 13, 128, 0.05), (600, 128, 1000, 10, 16, 0.0),
+         (257, 128, 513, 33, 64, 0.3), (9000, 128, 16, 8, 32, 0.1), (1800, 128, 1024, 9, 16, 0.2)]
 
 
 def _idx(T, E, k, dropped, seed=0):
