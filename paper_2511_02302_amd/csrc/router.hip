@@ -29,6 +29,7 @@ namespace ff8 {
 namespace {
 
 constexpr int kThreads = 256;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ---- reductions over the aligned group of L = 16 or 64 lanes (every lane gets the result) ----
 
@@ -461,8 +462,30 @@ __device__ __forceinline__ void spread_slot(int idx, float g, int k, int lane, f
     spread_slot<L, V, J + 1>(idx, g, k, lane, d);
   }
 }
+// From eight experts a lane on the sums are made in LDS (`row`: the group's L * V floats, a lane's four in a piece and
+// the lanes side by side): the slots' lanes add theirs one behind the other.
 template <int L, int V>
-__device__ __forceinline__ void spread(int idx, float g, int k, int lane, float (&d)[V]) {
+constexpr bool kSpreadInLds = L == 16 && V >= 8;
+template <int L, int V>
+__device__ __forceinline__ void spread(int idx, float g, int k, int lane, float* row, float (&d)[V]) {
+  if constexpr (kSpreadInLds<L, V>) {
+    f32x4* const pieces = reinterpret_cast<f32x4*>(row) + lane;
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) pieces[q * 16] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int i = idx < 0 ? 0 : idx, v = i % V;
+    float* const at = row + ((v / 4) * 16 + i / V) * 4 + v % 4;
+    for (int j = 0; j < k; ++j)
+      if (lane == j && idx >= 0) __hip_atomic_fetch_add(at, g, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+      const f32x4 p = pieces[q * 16];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) d[4 * q + u] = p[u];
+    }
+    return;
+  }
 #pragma unroll
   for (int v = 0; v < V; ++v) d[v] = 0.0f;
   if constexpr (L == 16) {
@@ -487,6 +510,8 @@ __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict_
   const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
   if (t >= T) return;
   const X* row = logits + t * E;
+  __shared__ __align__(16) float in_lds[kSpreadInLds<L, V> ? kThreads * V : 4];
+  float* const sums = in_lds + (kSpreadInLds<L, V> ? threadIdx.x / L * (L * V) : 0);
   float d[V];
   // slot `lane`: its expert (-1: none) and its weight's gradient
   int idx = lane < k ? topk_idx[t * k + lane] : -1;
@@ -512,7 +537,7 @@ __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict_
     }
     sum = group_sum<L>(sum);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    spread<L, V>(idx, g, k, lane, d);
+    spread<L, V>(idx, g, k, lane, sums, d);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       p[v] *= inv;
@@ -534,7 +559,7 @@ __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict_
     } else if (idx >= 0) {
       g = scale * g * sigmoid(l) * sigmoid(-l);
     }
-    spread<L, V>(idx, g, k, lane, d);
+    spread<L, V>(idx, g, k, lane, sums, d);
   }
   store_row<V>(dlogits + t * E, lane, E, vec, d);
 }
