@@ -13,8 +13,8 @@
 // and zero for experts that are not chosen in the last two.
 //
 // What bounds it.  The floor is one read of the logits (8.4 MB at 16384 tokens x 256 experts: 1.4 us, of which
-// the choice is measured at 8.0 and the gradient, 17.8 MB and 2.7 us, at 7.0: a launch alone is about 2 and the
-// rest is instructions).  So those are kept few: a token is held by 16 lanes (or by a wave, for few tokens or many
+// the choice with a bias is measured at 7.5 and the gradient, 17.8 MB and 2.7 us, at 6.2: a launch alone is about 2
+// and the rest is instructions).  So those are kept few: a token is held by 16 lanes (or by a wave, for few tokens or many
 // experts), its experts in registers, reductions run on DPP and lane swaps instead of LDS, bf16 logits carry
 // their expert's number in the low half of one word for the k rounds of the maximum, and where they cannot, the
 // candidates for the k places are found and ranked by counting.
@@ -222,7 +222,8 @@ __device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], 
   }
 }
 
-// The same by ranks, for 16 lanes (k <= 16), where that takes a fraction of the rounds' instructions: the k-th of the
+// The same by ranks, for 16 lanes (k <= 16), where that takes a fraction of the rounds' instructions (16384 x 256 biased
+// 7.5 us; over packed keys, whose rounds are short, ranks were no faster: 8.2 us against 7.9): the k-th of the
 // lanes' largest keys bounds the k-th of all from below; the keys from there on (11 of 256 for k = 8, on average) go
 // to the lanes in expert order, one each (two where a group of the wave has more than 16), and each lane counts the
 // better ones.  With a bias the candidates begin as far below that as float32 may be off, and where the order
@@ -462,8 +463,9 @@ __device__ __forceinline__ void spread_slot(int idx, float g, int k, int lane, f
     spread_slot<L, V, J + 1>(idx, g, k, lane, d);
   }
 }
-// From eight experts a lane on the sums are made in LDS (`row`: the group's L * V floats, a lane's four in a piece and
-// the lanes side by side): the slots' lanes add theirs one behind the other.
+// From eight experts a lane on the sums are made in LDS (`row`: the group's L * V floats, a lane's four in a piece
+// and the lanes side by side): the slots' lanes add theirs one behind the other.  16384 tokens x 256 experts 6.2 us, in
+// registers 7.3; x 96 experts 4.2 both ways.
 template <int L, int V>
 constexpr bool kSpreadInLds = L == 16 && V >= 8;
 template <int L, int V>
@@ -566,12 +568,12 @@ __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict_
 
 // Lanes a token.  Sixteen (four tokens a wave) take a quarter of the reductions of a whole wave but hold four
 // times the experts a lane.  The wave is for k above 16 (a lane holds a slot), for more than 256 experts, and for
-// few tokens where the experts are chosen by rounds over packed keys or there are none to choose (`rounds`: bf16
-// logits without a bias, the gradient), as a round's latency counts there: 256 experts, k = 8, 16 against 64 lanes,
-// us: 1 token 3.4 2.1, 64 4.2 3.2, 2048 4.6 3.6, 4096 4.5 4.6, 16384 8.0 10.4; gradient 2.9 2.0, 3.4 3.1, 4.0 3.3,
-// 4.4 4.2, 7.0 9.2.  Up to 64 experts sixteen are as fast or faster from 64 tokens on (64: 2.5 2.9, 16384: 4.2 8.0),
-// and so they are at any number where 16 lanes choose by ranks (1 token 2.9 3.1 in float32, 3.6 3.9 with a bias;
-// 2048 tokens 4.7 5.0 and 5.5 8.7).
+// few tokens where the experts are chosen by rounds over packed keys (`rounds`: bf16 logits without a bias), as a
+// round's latency counts there: 256 experts, k = 8, 16 against 64 lanes, us: 1 token 3.4 2.1, 64 4.1 3.2, 2048 4.4 3.6,
+// 4096 4.7 4.8, 16384 7.8 11.0.  Up to 64 experts sixteen are as fast or faster from 64 tokens on (64: 2.5 2.9,
+// 16384: 4.2 8.0), and so they are at any number where 16 lanes choose by ranks (1 token 2.9 3.1 in float32, 3.6
+// 3.9 with a bias; 2048 tokens 4.7 5.0 and 5.5 8.7) and in the gradient (1 token 2.2 2.4, of all logits 2.6 2.1,
+// 64 3.0 3.9, 3.1 2.9, 2048 3.4 3.5, 3.5 3.5, 16384 5.0 10.2, 5.0 9.4).
 int lanes_of(int64_t T, int E, int k, bool rounds) {
   if (E > 256 || k > 16) return 64;
   return rounds && E > 64 && T <= 2048 ? 64 : 16;
@@ -656,7 +658,7 @@ hipError_t topk_bwd_impl(const X* logits, const int32_t* idx, const float* dprob
                          bool norm, float scale, X* dlogits, hipStream_t st) {
   if (T == 0) return hipSuccess;
 #define FF8_CALL(L, V) topk_bwd_launch<L, V, X>(logits, idx, dprobs, T, E, k, sig, norm, scale, dlogits, st)
-  FF8_BY_SIZE(T, E, k, true, FF8_CALL)
+  FF8_BY_SIZE(T, E, k, false, FF8_CALL)
 #undef FF8_CALL
 }
 
