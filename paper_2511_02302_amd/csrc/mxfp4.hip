@@ -293,7 +293,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
 //
 // Bound by the matrix cores and the loads together: 32 experts with 32 rows on average, 7168 columns, 2 x 2048 rows
 // (511 MB): 131 to 138 us, 3.8 TB/s.  The loads alone take 94 us (74 at the rate of a large read), the matrix
-// instructions alone 101 (61 at that of a large product, 1370 TFLOP/s): experts' rows come in 16s, and one
+// instructions alone 101 (88 at that of a large product, 1370 TFLOP/s): experts' rows come in 16s, and one
 // CU's are not another's.  Together they draw the clock from 2.45 to 1.97 GHz, so that the sum of cycles stays
 // near the larger of the two and the time does not.  Blocks of 48 or 64 rows and weights three blocks
 // ahead were slower.

@@ -7,6 +7,9 @@ made by the scaling-aware transpose from the row-wise FP8 tensors already in mem
 BF16 stays only at the fc1 output (feeding the activation) and at the fc2 output
 (feeding the combine in the forward and the dispatch in the backward).
 
+`ExpertLayerFP4` at the end is the serving form: the forward from the router's logits, with
+4-bit weights and bf16 activations.
+
 Every step is one or more calls into libff8.so through the ctypes binding; torch
 only provides device memory and the stream.
 
