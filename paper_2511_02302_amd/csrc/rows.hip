@@ -9,11 +9,12 @@
 // Both are bound by HBM: one wave moves one row (16-byte pieces, consecutive lanes), eight waves a workgroup, so
 // that the k rows of a token are mostly written by one workgroup and its input row comes from HBM once and from
 // the XCD's L2 the other times.  A lane has up to eight pieces in flight before its first store.  At 16384
-// tokens x 7168 in bf16, k = 8 (2.1 GB) the sort takes 390 us, 5.4 TB/s: a workgroup per token that holds its row
+// tokens x 7168 in bf16, k = 8 (2.1 GB) the sort takes 386 us, 5.5 TB/s: a workgroup per token that holds its row
 // in registers took 422, loads that alternate with stores 410, a row per workgroup 516, a wave per output row in
-// output order 548.  The gradient (4.0 GB) takes 758 us, 5.3 TB/s (772 with a workgroup per token).  Copying the
+// output order 548.  The gradient (4.0 GB) takes 757 us, 5.3 TB/s (772 with a workgroup per token).  Copying the
 // same rows in order reaches 5.8 TB/s and in the sorted order 5.5, so what is left is the order that the routing
-// gives.  The first E workgroups of a launch fill the expert groups' padding rows.
+// gives.  Workgroups behind those fill the expert groups' padding rows: behind, so that they do not hold up the rows
+// (512 x 7168, 64 experts, k = 8, padded to 128: gradient 38 us, 45 with the padding first).
 // The routing maps are those of ff8_permute_quant.
 
 #include "ff8_device.hpp"
@@ -24,6 +25,7 @@ namespace ff8 {
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kPadGroups = 512;
 constexpr int kPieces = 8;  // 16-byte pieces that a lane has in flight
 
 // One wave: row r becomes token t's row, or a row of zeros (scales 2^-126).  row16: 16-byte pieces of a row; n_s:
@@ -55,7 +57,7 @@ __device__ __forceinline__ void clear_row(int64_t r, int lane, int64_t row16, in
 // Their numbers are collected in LDS first (two loads a lane instead of one before every row), then each wave
 // takes every eighth.
 template <typename S>
-__device__ __forceinline__ void pad_rows(int e, const int32_t* __restrict__ offsets, const int32_t* __restrict__ src_row,
+__device__ __forceinline__ void pad_rows(int e, int part, int parts, const int32_t* __restrict__ offsets, const int32_t* __restrict__ src_row,
                                          int64_t M_cap, int64_t row16, int n_s, u32x4* __restrict__ out,
                                          S* __restrict__ s_out) {
   __shared__ int rows[kTile];
@@ -76,34 +78,36 @@ __device__ __forceinline__ void pad_rows(int e, const int32_t* __restrict__ offs
     if (lane == 0) n_rows = n;
   }
   __syncthreads();
-  for (int i = threadIdx.x >> 6; i < n_rows; i += kWaves) clear_row<S>(r0 + rows[i], lane, row16, n_s, out, s_out);
+  for (int i = part * kWaves + (int)(threadIdx.x >> 6); i < n_rows; i += parts * kWaves)
+    clear_row<S>(r0 + rows[i], lane, row16, n_s, out, s_out);
 }
 
-// The (token, slot) pair of a wave behind the E padding workgroups; the same for all its lanes.
-__device__ __forceinline__ int pair_of_wave(int E) {
-  return __builtin_amdgcn_readfirstlane((int)(blockIdx.x - E) * kWaves + (int)(threadIdx.x >> 6));
+// The (token, slot) pair of a wave; the same for all its lanes.
+__device__ __forceinline__ int pair_of_wave() {
+  return __builtin_amdgcn_readfirstlane((int)blockIdx.x * kWaves + (int)(threadIdx.x >> 6));
 }
 
 template <typename S>
 __global__ __launch_bounds__(kThreads) void sort_rows_kernel(const u32x4* __restrict__ x, const S* __restrict__ s,
-                                                             int64_t row16, int n_s, int n_pairs, int k, int E,
+                                                             int64_t row16, int n_s, int n_pairs, int k, int parts,
                                                              const int32_t* __restrict__ row_map,
                                                              const int32_t* __restrict__ offsets,
                                                              const int32_t* __restrict__ src_row, int64_t M_cap,
                                                              u32x4* __restrict__ out, S* __restrict__ s_out) {
-  if ((int)blockIdx.x < E) {
-    pad_rows<S>((int)blockIdx.x, offsets, src_row, M_cap, row16, n_s, out, s_out);
+  const int pad = (int)blockIdx.x - (n_pairs + kWaves - 1) / kWaves;
+  if (pad >= 0) {
+    pad_rows<S>(pad / parts, pad % parts, parts, offsets, src_row, M_cap, row16, n_s, out, s_out);
     return;
   }
-  const int p = pair_of_wave(E), lane = threadIdx.x & 63;
+  const int p = pair_of_wave(), lane = threadIdx.x & 63;
   if (p >= n_pairs) return;
   const int64_t t = p / k, r = row_map[p];
   if (r >= 0 && r < M_cap) move_row<S>(x, s, t, r, lane, row16, n_s, out, s_out);
 }
 
 // Routing and rows in one launch: a workgroup takes kWaves * kPer (token, slot) pairs, finds the pairs of each
-// expert and those before its own, and so knows the group offsets and its rows.  Behind those, one workgroup an
-// expert fills the group's padding.  Integer LDS atomics: the counts do not depend on order.
+// expert and those before its own, and so knows the group offsets and its rows.  Behind those, others fill the
+// expert groups' padding.  Integer LDS atomics: the counts do not depend on order.
 // Up to kMaxPairs pairs every workgroup counts them all by itself.  us, so / with the routing in launches of its own:
 // 1024 tokens x 256 columns, 8 experts, k = 2 6.9 / 11.4; 512 x 7168, 64 experts, k = 8 17 / 26, with 128-row padding
 // 29 / 38; 4096 x 256, 1024 experts, k = 1 10.4 / 12.7.  (8192 x 256, 8 experts, k = 1 14.8 / 12.6.)
@@ -129,7 +133,7 @@ __global__ __launch_bounds__(kThreads) void chunk_count_kernel(const int32_t* __
 template <typename S, int kPer>
 __global__ __launch_bounds__(kThreads) void route_sort_kernel(
     const u32x4* __restrict__ x, const S* __restrict__ s, const int32_t* __restrict__ topk_idx, int n_pairs, int k, int E,
-    int align, const int32_t* __restrict__ counts, int n_chunks, int64_t row16, int n_s, int64_t M_cap,
+    int align, int parts, const int32_t* __restrict__ counts, int n_chunks, int64_t row16, int n_s, int64_t M_cap,
     int32_t* __restrict__ row_map, int32_t* __restrict__ offsets, int32_t* __restrict__ src_row,
     u32x4* __restrict__ out, S* __restrict__ s_out) {
   __shared__ int total[kMaxExperts], before[kMaxExperts];  // pairs of an expert, and those before the workgroup's
@@ -137,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void route_sort_kernel(
   constexpr int kBlock = kWaves * kPer;
   static_assert(kBlock <= 64, "a lane holds a pair");
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n_sort = (n_pairs + kBlock - 1) / kBlock, pad = (int)blockIdx.x - n_sort;  // pad: the expert, or below 0
+  const int n_sort = (n_pairs + kBlock - 1) / kBlock, pad = (int)blockIdx.x - n_sort;  // below 0: rows
   const int p0 = pad < 0 ? (int)blockIdx.x * kBlock : 0;
   const int mine = lane < kBlock && p0 + lane < n_pairs ? topk_idx[p0 + lane] : -1;
   for (int e = tid; e < E; e += kThreads) {
@@ -213,8 +217,9 @@ __global__ __launch_bounds__(kThreads) void route_sort_kernel(
       move_row<S>(x, s, p / k, r, lane, row16, n_s, out, s_out);
     }
   } else {
-    const int64_t r1 = start[pad + 1] < M_cap ? start[pad + 1] : M_cap;
-    for (int64_t r = start[pad] + total[pad] + wave; r < r1; r += kWaves) {
+    const int e = pad / parts, part = pad - e * parts;
+    const int64_t r1 = start[e + 1] < M_cap ? start[e + 1] : M_cap;
+    for (int64_t r = start[e] + total[e] + part * kWaves + wave; r < r1; r += parts * kWaves) {
       if (lane == 0) src_row[r] = -1;
       clear_row<S>(r, lane, row16, n_s, out, s_out);
     }
@@ -224,14 +229,15 @@ __global__ __launch_bounds__(kThreads) void route_sort_kernel(
 // Sum of a dot product, fixed order: a lane's products in column order, then a butterfly over the wave.
 template <bool kDprobs>
 __global__ __launch_bounds__(kThreads) void return_bwd_kernel(
-    const u32x4* __restrict__ dy, const float* __restrict__ row_w, int64_t row16, int n_pairs, int k, int E,
+    const u32x4* __restrict__ dy, const float* __restrict__ row_w, int64_t row16, int n_pairs, int k, int parts,
     const int32_t* __restrict__ row_map, const int32_t* __restrict__ offsets, const int32_t* __restrict__ src_row,
     int64_t M_cap, u32x4* __restrict__ dy_perm, const u32x4* __restrict__ y_perm, float* __restrict__ dprobs) {
-  if ((int)blockIdx.x < E) {
-    pad_rows<e8m0_t>((int)blockIdx.x, offsets, src_row, M_cap, row16, 0, dy_perm, nullptr);
+  const int pad = (int)blockIdx.x - (n_pairs + kWaves - 1) / kWaves;
+  if (pad >= 0) {
+    pad_rows<e8m0_t>(pad / parts, pad % parts, parts, offsets, src_row, M_cap, row16, 0, dy_perm, nullptr);
     return;
   }
-  const int p = pair_of_wave(E), lane = threadIdx.x & 63;
+  const int p = pair_of_wave(), lane = threadIdx.x & 63;
   if (p >= n_pairs) return;
   const int64_t t = p / k, r = row_map[p];
   float acc = 0.0f;
@@ -278,7 +284,15 @@ bool counted(int64_t n_pairs, int64_t n_counts, int64_t row16) {
   return n_pairs <= (row16 >= 256 ? 48 << 10 : 32 << 10) && n_pairs * n_counts <= (int64_t)1 << 27;
 }
 
-unsigned grid_of(int64_t n_pairs, int E) { return (unsigned)(E + (n_pairs + kWaves - 1) / kWaves); }
+// Workgroups for an expert's padding (up to align - 1 rows of zeros): a wave a row, as long as there are no more than
+// kPadGroups, and one for rows below 2 KiB.  us, so / one each: 34 tokens x 6144, 24 experts, k = 7, padded to 128 9.5 /
+// 16.6; 199 x 4608, 27, k = 2 8.6 / 13.3; 300 x 1024, 8, k = 2 7.2 / 7.2.  With 256 at the most 9.8 and 8.7.
+int pad_parts(int E, int align, int64_t row16) {
+  const int most = E < kPadGroups ? kPadGroups / E : 1, need = align / kWaves;
+  return row16 < 128 ? 1 : most < need ? most : need;
+}
+
+unsigned grid_of(int64_t n_pairs, int n_pad) { return (unsigned)(n_pad + (n_pairs + kWaves - 1) / kWaves); }
 
 // With topk_idx the routing maps are built too.
 template <typename S>
@@ -288,12 +302,13 @@ hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_
   const u32x4* const in = static_cast<const u32x4*>(x);
   u32x4* const to = static_cast<u32x4*>(out);
   const int64_t n_pairs = T * k;
+  const int parts = pad_parts(E, topk_idx ? align : kTile, row16);  // (maps that are there may have any padding)
   if (topk_idx || T == 0) {
     const int64_t n_chunks = (T + kChunk - 1) / kChunk;
     int32_t* const counts = static_cast<int32_t*>(workspace);
 #define FF8_GO(PER, COUNTS)                                                                                         \
-  route_sort_kernel<S, PER><<<(unsigned)(E + (n_pairs + kWaves * PER - 1) / (kWaves * PER)), kThreads, 0, st>>>(    \
-      in, s, topk_idx, (int)n_pairs, k, E, align, COUNTS, (int)n_chunks, row16, n_s, M_cap, row_map, offsets, \
+  route_sort_kernel<S, PER><<<(unsigned)(E * parts + (n_pairs + kWaves * PER - 1) / (kWaves * PER)), kThreads, 0, st>>>(    \
+      in, s, topk_idx, (int)n_pairs, k, E, align, parts, COUNTS, (int)n_chunks, row16, n_s, M_cap, row_map, offsets, \
       src_row, to, s_out)
     if (n_pairs <= kMaxPairs) {
       FF8_GO(1, nullptr);
@@ -308,8 +323,8 @@ hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_
     const hipError_t e = launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace, st);
     if (e != hipSuccess) return e;
   }
-  sort_rows_kernel<S><<<grid_of(n_pairs, E), kThreads, 0, st>>>(in, s, row16, n_s, (int)n_pairs, k, E, row_map, offsets,
-                                                                src_row, M_cap, to, s_out);
+  sort_rows_kernel<S><<<grid_of(n_pairs, E * parts), kThreads, 0, st>>>(in, s, row16, n_s, (int)n_pairs, k, parts,
+                                                                        row_map, offsets, src_row, M_cap, to, s_out);
   return hipGetLastError();
 }
 
@@ -337,14 +352,15 @@ hipError_t launch_permute_fp8(const uint8_t* xq, const e8m0_t* xs, int64_t T, in
 hipError_t launch_unpermute_bwd(const uint16_t* dy, const float* row_w, int64_t T, int64_t H, int k, int E,
                                 const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
                                 uint16_t* dy_perm, const uint16_t* y_perm, float* dprobs, hipStream_t st) {
-  const unsigned grid = grid_of(T * k, E);
+  const int parts = pad_parts(E, kTile, H / 8);
+  const unsigned grid = grid_of(T * k, E * parts);
   const u32x4 *d = reinterpret_cast<const u32x4*>(dy), *y = reinterpret_cast<const u32x4*>(y_perm);
   u32x4* const o = reinterpret_cast<u32x4*>(dy_perm);
   if (dprobs)
-    return_bwd_kernel<true><<<grid, kThreads, 0, st>>>(d, row_w, H / 8, (int)(T * k), k, E, row_map, offsets, src_row,
+    return_bwd_kernel<true><<<grid, kThreads, 0, st>>>(d, row_w, H / 8, (int)(T * k), k, parts, row_map, offsets, src_row,
                                                        M_cap, o, y, dprobs);
   else
-    return_bwd_kernel<false><<<grid, kThreads, 0, st>>>(d, row_w, H / 8, (int)(T * k), k, E, row_map, offsets, src_row,
+    return_bwd_kernel<false><<<grid, kThreads, 0, st>>>(d, row_w, H / 8, (int)(T * k), k, parts, row_map, offsets, src_row,
                                                         M_cap, o, nullptr, nullptr);
   return hipGetLastError();
 }
