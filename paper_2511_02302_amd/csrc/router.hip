@@ -88,6 +88,9 @@ __device__ __forceinline__ float to_f32(uint16_t v) { return __uint_as_float((ui
 __device__ __forceinline__ void from_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void from_f32(uint16_t* p, float v) { *p = (uint16_t)f32_to_bf16(v); }
 
+// How a row's experts are moved: one by one, in a lane's pieces, or through LDS.
+enum class Rows { kSingle, kPieces, kStaged };
+
 // vec: E is a multiple of V and the tensor is aligned to a lane's piece (at most 16 bytes), so a lane's experts
 // are all there or all missing.
 template <int V, typename X>
@@ -131,6 +134,50 @@ __device__ __forceinline__ void store_row(X* row, int lane, int E, bool vec, con
     for (int v = 0; v < V; ++v)
       if (lane * V + v < E) row[lane * V + v] = x[v];
   }
+}
+
+// Rows that are not aligned to a lane's piece (E no multiple of it) go through LDS: the 16 rows of a workgroup are
+// one run of memory that begins at a multiple of 16 bytes, so they are moved in whole pieces, and a lane takes its
+// experts from LDS.  One by one, an access meets 16 lines and more for 64 elements.
+constexpr int kStagedRows = kThreads / 16;
+template <int L, int V>
+constexpr bool kCanStage = L == 16 && V >= 8;
+extern __shared__ u32x4 stage[];  // where rows are staged: kThreads * V elements, and 16 * V of the bias
+
+// The workgroup's elements, from global memory to LDS or back.
+template <typename X>
+__device__ __forceinline__ void move_staged(const X* from, X* to, int n) {
+  constexpr int kPer = 16 / sizeof(X);
+  for (int i = (int)threadIdx.x * kPer; i + kPer <= n; i += kThreads * kPer)
+    *reinterpret_cast<u32x4*>(to + i) = *reinterpret_cast<const u32x4*>(from + i);
+  const int i = n / kPer * kPer + (int)threadIdx.x;
+  if (i < n) to[i] = from[i];
+}
+__device__ __forceinline__ int staged_elements(int64_t T, int E) {
+  const int64_t left = T - (int64_t)blockIdx.x * kStagedRows;
+  return (int)(left < kStagedRows ? left : kStagedRows) * E;
+}
+
+// Experts a lane holds, from per * lane on: V in pieces, otherwise as many as spread them over all 16 lanes.  Where the
+// experts are chosen by ranks they are spread, and so staged, up to 10 V too: with few lanes the lanes' largest keys
+// are a poor bound for the candidates.  By E alone, so that results do not depend on the address.
+// 16384 tokens with a bias, k = 8, us, staged / in pieces: 144 experts 8.5 / 12.0, 160 8.7 / 10.5, 192 9.0 / 9.0, 256 7.9 /
+// 7.5; over packed keys 160 8.6 / 8.0, the gradient 6.4 / 5.0.  And staged and spread / one by one: 129 8.5 / 21.8, 255 9.3 /
+// 18.6, the gradient 7.6 / 20.2; 49 experts (V = 4) 7.0 / 7.3 and 4.5 / 4.5.
+template <int L, int V>
+__host__ __device__ __forceinline__ int experts_per_lane(int E, bool ranked) {
+  return kCanStage<L, V> && (E % V != 0 || (ranked && E <= 10 * V)) ? (E + 15) / 16 : V;
+}
+template <int V, typename X>
+__device__ __forceinline__ void load_experts(const X* row, int lane, int per, int E, X missing, X (&x)[V]) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) x[v] = v < per && lane * per + v < E ? row[lane * per + v] : missing;
+}
+template <int V, typename X>
+__device__ __forceinline__ void store_experts(X* row, int lane, int per, int E, const float (&d)[V]) {
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if (v < per && lane * per + v < E) from_f32(&row[lane * per + v], d[v]);
 }
 
 // ---- scores ----
@@ -190,7 +237,7 @@ __device__ __forceinline__ bool certain(const Choice& a, const Choice& b, float 
 // k rounds over keys of type K (-inf: never chosen): the largest of the group, the lowest lane that has it, its
 // lowest expert.  Slot j of `out` is written by the lane that held it; chosen keys become -inf.
 template <int L, int V, typename K, typename Out>
-__device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], int k, Out& out) {
+__device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], int per, int k, Out& out) {
   const int lane = threadIdx.x & (L - 1), base = threadIdx.x & 63 & ~(L - 1);
   for (int j = 0; j < k; ++j) {
     K best = key[0];
@@ -218,7 +265,7 @@ __device__ __forceinline__ void choose_rounds(K (&key)[V], const float (&l)[V], 
       key[v] = hit ? (K)-INFINITY : key[v];
       mine = mine && !hit;
     }
-    if (lane == win) out.put(j, {top > -INFINITY ? lane * V + at : -1, logit, (float)top, 0.0f});
+    if (lane == win) out.put(j, {top > -INFINITY ? lane * per + at : -1, logit, (float)top, 0.0f});
   }
 }
 
@@ -290,8 +337,8 @@ __device__ __forceinline__ double row_sum64(const float (&l)[V], float m) {
   return z;
 }
 template <int V, bool kSigmoid, bool kBias, typename Out>
-__device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float (&l)[V], const float* b, int k,
-                                              float err, float m, Out& out) {
+__device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float (&l)[V], const float* b, int per,
+                                              int k, float err, float m, Out& out) {
   const int lane = threadIdx.x & 15;
   float best = key[0];
 #pragma unroll
@@ -308,7 +355,7 @@ __device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float
   int at = end - n;
 #pragma unroll
   for (int v = 0; v < V; ++v)
-    if (key[v] >= bound) out.put(at++, {lane * V + v, l[v], key[v], kBias ? b[v] : 0.0f});
+    if (key[v] >= bound) out.put(at++, {lane * per + v, l[v], key[v], kBias ? b[v] : 0.0f});
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   Choice c = {-1, -INFINITY, -INFINITY, 0.0f}, d = c;
   if (lane < total) c = out.get(lane);
@@ -340,7 +387,7 @@ __device__ __forceinline__ bool choose_ranked(const float (&key)[V], const float
 
 template <int L, int V, bool kSigmoid, bool kNormalize, bool kBias, typename X>
 __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ logits, const float* __restrict__ bias,
-                                                        int64_t T, int E, int k, float scale, bool vec,
+                                                        int64_t T, int E, int k, float scale, Rows rows,
                                                         bool vec_bias, int32_t* __restrict__ topk_idx, float* __restrict__ probs) {
   constexpr bool kPacked = sizeof(X) == 2 && !kBias;
   constexpr bool kFull = !kSigmoid && (kBias || !kNormalize);  // the softmax over all experts is needed
@@ -349,10 +396,25 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
   const int lane = threadIdx.x & (L - 1);
   Choices<kFound>& mine = found[kPacked ? 0 : threadIdx.x / L];
   const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
-  if (t >= T) return;  // whole groups of L lanes
   X raw[V], missing;
   from_f32(&missing, -INFINITY);
-  load_row<V>(logits + t * E, lane, E, vec, missing, raw);
+  const bool staged = kCanStage<L, V> && rows == Rows::kStaged;
+  const int per = experts_per_lane<L, V>(E, !kPacked);
+  float* const bias_stage = reinterpret_cast<float*>(reinterpret_cast<X*>(stage) + kThreads * V);
+  if (staged) {
+    X* const in = reinterpret_cast<X*>(stage);
+    move_staged(logits + (int64_t)blockIdx.x * kStagedRows * E, in, staged_elements(T, E));
+    if (kBias && (int)threadIdx.x < E) bias_stage[threadIdx.x] = bias[threadIdx.x];
+    __syncthreads();
+    load_experts<V>(in + threadIdx.x / L * E, lane, per, E, missing, raw);
+  }
+  if (t >= T) return;  // whole groups of L lanes
+  if (!staged) {
+    if (kCanStage<L, V> && rows == Rows::kSingle)
+      load_experts<V>(logits + t * E, lane, per, E, missing, raw);
+    else
+      load_row<V>(logits + t * E, lane, E, rows == Rows::kPieces, missing, raw);
+  }
   float l[V], m = 0.0f, sum = 1.0f, e[kFull ? V : 1];
 #pragma unroll
   for (int v = 0; v < V; ++v) l[v] = to_f32(raw[v]);
@@ -374,7 +436,7 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
   if constexpr (kPacked) {
     uint32_t key[V], word = 0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = packed_key(raw[v], lane * V + v);
+    for (int v = 0; v < V; ++v) key[v] = packed_key(raw[v], lane * per + v);
     for (int j = 0; j < k; ++j) {
       uint32_t top = key[0];
 #pragma unroll
@@ -390,15 +452,18 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
     if (!kBias) {
 #pragma unroll
       for (int v = 0; v < V; ++v) key[v] = l[v] > -INFINITY ? l[v] : -INFINITY;  // NaN is never chosen
-      if (L != 16 || !choose_ranked<V, kSigmoid, false>(key, l, nullptr, k, 0.0f, 0.0f, mine))
-        choose_rounds<L, V>(key, l, k, mine);
+      if (L != 16 || !choose_ranked<V, kSigmoid, false>(key, l, nullptr, per, k, 0.0f, 0.0f, mine))
+        choose_rounds<L, V>(key, l, per, k, mine);
     } else {
       // In float32 first.  Both scores are off by less than 2^-21 (sigmoid: the exponential's and the
       // reciprocal's unit, damped) or 2^-18 of the row's largest (softmax: a sum of up to 1024), the sum by
       // half a unit; `err` is over twice that.  What float32 does not tell is decided in float64.
       const float inv = 1.0f / sum;
       float b[V];
-      load_row<V>(bias, lane, E, vec_bias, 0.0f, b);
+      if (staged || (kCanStage<L, V> && rows == Rows::kSingle))
+        load_experts<V>(staged ? bias_stage : bias, lane, per, E, 0.0f, b);
+      else
+        load_row<V>(bias, lane, E, vec_bias, 0.0f, b);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const float s = kSigmoid ? __builtin_amdgcn_rcpf(1.0f + __expf(-l[v])) : e[kFull ? v : 0] * inv;
@@ -406,8 +471,8 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
         key[v] = ((l[v] > -INFINITY) & (sum_b > -INFINITY)) ? sum_b : -INFINITY;
       }
       const float err = kSigmoid ? 0x1p-19f : 0x1p-16f * inv;
-      if (L != 16 || !choose_ranked<V, kSigmoid, true>(key, l, b, k, err, m, mine)) {
-        choose_rounds<L, V>(key, l, k, mine);
+      if (L != 16 || !choose_ranked<V, kSigmoid, true>(key, l, b, per, k, err, m, mine)) {
+        choose_rounds<L, V>(key, l, per, k, mine);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         bool unsure = false;
         auto of = [&](int j) {
@@ -420,14 +485,14 @@ __global__ __launch_bounds__(kThreads) void topk_kernel(const X* __restrict__ lo
           const Choice last = of(k - 1);
 #pragma unroll
           for (int v = 0; v < V; ++v)
-            unsure |= (key[v] > -INFINITY) & !certain(last, {lane * V + v, l[v], key[v], b[v]}, err);
+            unsure |= (key[v] > -INFINITY) & !certain(last, {lane * per + v, l[v], key[v], b[v]}, err);
         }
         if (__any(unsure)) {
           const double z = row_sum64<L, V, kSigmoid>(l, m);
           double wide[V];
 #pragma unroll
           for (int v = 0; v < V; ++v) wide[v] = key64<kSigmoid>(l[v], b[v], m, z);  // a missing expert's l is -inf
-          choose_rounds<L, V>(wide, l, k, mine);
+          choose_rounds<L, V>(wide, l, per, k, mine);
         }
       }
     }
@@ -469,14 +534,14 @@ __device__ __forceinline__ void spread_slot(int idx, float g, int k, int lane, f
 template <int L, int V>
 constexpr bool kSpreadInLds = L == 16 && V >= 8;
 template <int L, int V>
-__device__ __forceinline__ void spread(int idx, float g, int k, int lane, float* row, float (&d)[V]) {
+__device__ __forceinline__ void spread(int idx, float g, int k, int lane, int per, float* row, float (&d)[V]) {
   if constexpr (kSpreadInLds<L, V>) {
     f32x4* const pieces = reinterpret_cast<f32x4*>(row) + lane;
 #pragma unroll
     for (int q = 0; q < V / 4; ++q) pieces[q * 16] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int i = idx < 0 ? 0 : idx, v = i % V;
-    float* const at = row + ((v / 4) * 16 + i / V) * 4 + v % 4;
+    const int i = idx < 0 ? 0 : idx, owner = (int)((unsigned)i / (unsigned)per), v = i - owner * per;
+    float* const at = row + ((v / 4) * 16 + owner) * 4 + v % 4;
     for (int j = 0; j < k; ++j)
       if (lane == j && idx >= 0) __hip_atomic_fetch_add(at, g, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -506,11 +571,24 @@ template <int L, int V, bool kSigmoid, bool kNormalize, typename X>
 __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict__ logits,
                                                             const int32_t* __restrict__ topk_idx,
                                                             const float* __restrict__ dprobs, int64_t T, int E, int k,
-                                                            float scale, bool vec, X* __restrict__ dlogits) {
+                                                            float scale, Rows rows, X* __restrict__ dlogits) {
   constexpr bool kDense = !kSigmoid && !kNormalize;
   const int lane = threadIdx.x & (L - 1);
-  const int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
-  if (t >= T) return;
+  int64_t t = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+  const bool staged = kCanStage<L, V> && rows == Rows::kStaged;
+  const int per = experts_per_lane<L, V>(E, false);
+  X* const in_stage = reinterpret_cast<X*>(stage);
+  const int64_t first = (int64_t)blockIdx.x * kStagedRows * E;  // (staged)
+  if (staged) {  // the last workgroup's missing rows go along as the last row
+    if (kDense) {
+      move_staged(logits + first, in_stage, staged_elements(T, E));
+      __syncthreads();
+    }
+  } else if (t >= T) {
+    return;
+  }
+  const int local = (int)(t < T ? threadIdx.x / L : T - 1 - (t - threadIdx.x / L));  // row of the workgroup
+  t = t < T ? t : T - 1;
   const X* row = logits + t * E;
   __shared__ __align__(16) float in_lds[kSpreadInLds<L, V> ? kThreads * V : 4];
   float* const sums = in_lds + (kSpreadInLds<L, V> ? threadIdx.x / L * (L * V) : 0);
@@ -523,7 +601,10 @@ __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict_
   if (kDense) {
     X raw[V], missing;
     from_f32(&missing, -INFINITY);
-    load_row<V>(row, lane, E, vec, missing, raw);
+    if (staged || (kCanStage<L, V> && rows == Rows::kSingle))
+      load_experts<V>(staged ? in_stage + local * E : row, lane, per, E, missing, raw);
+    else
+      load_row<V>(row, lane, E, rows == Rows::kPieces, missing, raw);
     float p[V], m = -INFINITY, sum = 0.0f, dot = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -539,7 +620,7 @@ __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict_
     }
     sum = group_sum<L>(sum);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    spread<L, V>(idx, g, k, lane, sums, d);
+    spread<L, V>(idx, g, k, lane, per, sums, d);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       p[v] *= inv;
@@ -561,9 +642,18 @@ __global__ __launch_bounds__(kThreads) void topk_bwd_kernel(const X* __restrict_
     } else if (idx >= 0) {
       g = scale * g * sigmoid(l) * sigmoid(-l);
     }
-    spread<L, V>(idx, g, k, lane, sums, d);
+    spread<L, V>(idx, g, k, lane, per, sums, d);
   }
-  store_row<V>(dlogits + t * E, lane, E, vec, d);
+  if (staged) {
+    __syncthreads();
+    store_experts<V>(in_stage + local * E, lane, per, E, d);
+    __syncthreads();
+    move_staged<X>(in_stage, dlogits + first, staged_elements(T, E));
+  } else if (kCanStage<L, V> && rows == Rows::kSingle) {
+    store_experts<V>(dlogits + t * E, lane, per, E, d);
+  } else {
+    store_row<V>(dlogits + t * E, lane, E, rows == Rows::kPieces, d);
+  }
 }
 
 // Lanes a token.  Sixteen (four tokens a wave) take a quarter of the reductions of a whole wave but hold four
@@ -600,17 +690,31 @@ bool vector_rows(int E, const void* a, const void* b) {
   return E % V == 0 && (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % kBytes == 0;
 }
 
+// (every row of a tensor in the same way; LDS that a launch needs for it)
+template <int L, int V, typename X>
+Rows rows_of(int E, bool ranked, const void* a, const void* b) {
+  const bool aligned = (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % 16 == 0;
+  if (experts_per_lane<L, V>(E, ranked) == V && vector_rows<V, X>(E, a, b)) return Rows::kPieces;
+  return kCanStage<L, V> && aligned ? Rows::kStaged : Rows::kSingle;
+}
+template <int V, typename X>
+unsigned stage_bytes(Rows rows) {
+  return rows == Rows::kStaged ? (unsigned)(kThreads * V * sizeof(X) + 16 * V * sizeof(float)) : 0u;
+}
+
 template <int L, int V, typename X>
 hipError_t topk_launch(const X* logits, const float* bias, int64_t T, int E, int k, bool sig, bool norm, float scale,
                        int32_t* idx, float* probs, hipStream_t st) {
   const unsigned grid = (unsigned)((T + kThreads / L - 1) / (kThreads / L));
-  const bool vec = vector_rows<V, X>(E, logits, nullptr), vec_bias = vector_rows<V, float>(E, bias, nullptr);
+  const Rows rows = rows_of<L, V, X>(E, bias || sizeof(X) != 2, logits, nullptr);
+  const bool vec_bias = vector_rows<V, float>(E, bias, nullptr);
+  const unsigned lds = stage_bytes<V, X>(rows);
 #define FF8_GO(S, N)                                                                                               \
   if (bias)                                                                                                        \
-    topk_kernel<L, V, S, N, true, X><<<grid, kThreads, 0, st>>>(logits, bias, T, E, k, scale, vec, vec_bias, idx,  \
+    topk_kernel<L, V, S, N, true, X><<<grid, kThreads, lds, st>>>(logits, bias, T, E, k, scale, rows, vec_bias, idx,  \
                                                                 probs);                                            \
   else                                                                                                             \
-    topk_kernel<L, V, S, N, false, X><<<grid, kThreads, 0, st>>>(logits, bias, T, E, k, scale, vec, false, idx,    \
+    topk_kernel<L, V, S, N, false, X><<<grid, kThreads, lds, st>>>(logits, bias, T, E, k, scale, rows, false, idx,    \
                                                                  probs);
   if (sig && norm) {
     FF8_GO(true, true)
@@ -629,9 +733,10 @@ template <int L, int V, typename X>
 hipError_t topk_bwd_launch(const X* logits, const int32_t* idx, const float* dprobs, int64_t T, int E, int k, bool sig,
                            bool norm, float scale, X* dlogits, hipStream_t st) {
   const unsigned grid = (unsigned)((T + kThreads / L - 1) / (kThreads / L));
-  const bool vec = vector_rows<V, X>(E, logits, dlogits);
+  const Rows rows = rows_of<L, V, X>(E, false, logits, dlogits);
+  const unsigned lds = stage_bytes<V, X>(rows);
 #define FF8_GO(S, N) \
-  topk_bwd_kernel<L, V, S, N, X><<<grid, kThreads, 0, st>>>(logits, idx, dprobs, T, E, k, scale, vec, dlogits)
+  topk_bwd_kernel<L, V, S, N, X><<<grid, kThreads, lds, st>>>(logits, idx, dprobs, T, E, k, scale, rows, dlogits)
   if (sig && norm)
     FF8_GO(true, true);
   else if (sig)

@@ -14,7 +14,8 @@ pytestmark = pytest.mark.gpu
 MODES = [("softmax", False), ("softmax", True), ("sigmoid", False), ("sigmoid", True)]
 SHAPES = [(1, 1, 1), (3, 2, 2), (257, 5, 3), (64, 8, 2), (33, 16, 16), (70, 17, 17), (129, 32, 8), (65, 33, 1),
           (40, 64, 64), (31, 65, 64), (66, 100, 6), (9, 128, 8), (130, 160, 6), (12, 255, 9), (50, 256, 8),
-          (21, 257, 33), (7, 384, 8), (18, 512, 8), (6, 513, 12), (11, 1000, 64), (10, 1024, 8)]
+          (21, 257, 33), (7, 384, 8), (18, 512, 8), (6, 513, 12), (11, 1000, 64), (10, 1024, 8),
+          (37, 129, 8), (40, 130, 7), (50, 144, 8), (2100, 201, 3), (33, 160, 16), (70, 80, 5), (71, 66, 4)]
 
 
 def _logits(T, E, dtype, seed, std=2.0):
