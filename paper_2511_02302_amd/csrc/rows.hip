@@ -26,6 +26,10 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kPadGroups = 512;
+// Rows of at most kNarrow pieces are moved kNarrowRows at a time by a wave.  us, so / one a wave, maps there and maps to be
+// built: 16000 tokens x 128 columns, 8 experts, k = 8 10.1 / 27.1 and 21 / 38, gradient 26.5 / 46; x 512, 32 experts 25.6 / 29.7,
+// 39 / 42, 53 / 58.  (Wider ones four or two at a time: 1024 columns 49 / 44, 2048 98 / 97.)
+constexpr int kNarrow = 64, kNarrowRows = 8;
 constexpr int kPieces = 8;  // 16-byte pieces that a lane has in flight
 
 // One wave: row r becomes token t's row, or a row of zeros (scales 2^-126).  row16: 16-byte pieces of a row; n_s:
@@ -44,6 +48,42 @@ __device__ __forceinline__ void move_row(const u32x4* __restrict__ x, const S* _
       if (c0 + 64 * i < row16) stnt16(out + r * row16 + c0 + 64 * i, v[i]);
   }
   for (int c = lane; c < n_s; c += 64) s_out[r * n_s + c] = s[t * n_s + c];
+}
+// The same for kNarrowRows narrow rows at a time, so that a lane has as many pieces in flight as with long ones: row r[j]
+// becomes token t[j]'s, with r[j] = -1 none.  Loads are not behind conditions (t[j] is a token in any case; missing lanes
+// take the first piece): with branches between them every row waits for the one before.
+template <typename S>
+__device__ __forceinline__ void move_narrow(const u32x4* __restrict__ x, const S* __restrict__ s,
+                                            const int (&t)[kNarrowRows], const int (&r)[kNarrowRows], int lane,
+                                            int64_t row16, int n_s, u32x4* __restrict__ out, S* __restrict__ s_out) {
+  u32x4 v[kNarrowRows];
+  S sv[kNarrowRows];
+  const int piece = lane < row16 ? lane : 0;
+#pragma unroll
+  for (int j = 0; j < kNarrowRows; ++j) v[j] = ld16(x + t[j] * row16 + piece);
+  if (n_s) {
+#pragma unroll
+    for (int j = 0; j < kNarrowRows; ++j) sv[j] = s[(int64_t)t[j] * n_s + (lane < n_s ? lane : 0)];
+  }
+#pragma unroll
+  for (int j = 0; j < kNarrowRows; ++j)
+    if (r[j] >= 0 && lane < row16) stnt16(out + r[j] * row16 + lane, v[j]);
+#pragma unroll
+  for (int j = 0; j < kNarrowRows; ++j)
+    if (r[j] >= 0 && lane < n_s) s_out[(int64_t)r[j] * n_s + lane] = sv[j];
+}
+// Rows and tokens of the kNarrowRows pairs from p on (p < n_pairs); r = -1 for dropped pairs and behind the last.
+__device__ __forceinline__ void narrow_pairs(int p, int n_pairs, int k, int64_t M_cap, const int32_t* __restrict__ row_map,
+                                             int lane, int (&t)[kNarrowRows], int (&r)[kNarrowRows]) {
+  const int mine = p + lane % kNarrowRows, q = mine < n_pairs ? mine : n_pairs - 1;
+  int rq = row_map[q];
+  if (rq >= M_cap || mine >= n_pairs) rq = -1;
+  const int tq = q / k;
+#pragma unroll
+  for (int j = 0; j < kNarrowRows; ++j) {
+    r[j] = __builtin_amdgcn_readlane(rq, j);
+    t[j] = __builtin_amdgcn_readlane(tq, j);
+  }
 }
 template <typename S>
 __device__ __forceinline__ void clear_row(int64_t r, int lane, int64_t row16, int n_s, u32x4* __restrict__ out,
@@ -87,22 +127,29 @@ __device__ __forceinline__ int pair_of_wave() {
   return __builtin_amdgcn_readfirstlane((int)blockIdx.x * kWaves + (int)(threadIdx.x >> 6));
 }
 
-template <typename S>
+template <typename S, bool kIsNarrow>
 __global__ __launch_bounds__(kThreads) void sort_rows_kernel(const u32x4* __restrict__ x, const S* __restrict__ s,
                                                              int64_t row16, int n_s, int n_pairs, int k, int parts,
                                                              const int32_t* __restrict__ row_map,
                                                              const int32_t* __restrict__ offsets,
                                                              const int32_t* __restrict__ src_row, int64_t M_cap,
                                                              u32x4* __restrict__ out, S* __restrict__ s_out) {
-  const int pad = (int)blockIdx.x - (n_pairs + kWaves - 1) / kWaves;
+  constexpr int kBlock = kWaves * (kIsNarrow ? kNarrowRows : 1);
+  const int pad = (int)blockIdx.x - (n_pairs + kBlock - 1) / kBlock;
   if (pad >= 0) {
     pad_rows<S>(pad / parts, pad % parts, parts, offsets, src_row, M_cap, row16, n_s, out, s_out);
     return;
   }
-  const int p = pair_of_wave(), lane = threadIdx.x & 63;
+  const int p = pair_of_wave() * (kIsNarrow ? kNarrowRows : 1), lane = threadIdx.x & 63;
   if (p >= n_pairs) return;
-  const int64_t t = p / k, r = row_map[p];
-  if (r >= 0 && r < M_cap) move_row<S>(x, s, t, r, lane, row16, n_s, out, s_out);
+  if (kIsNarrow) {
+    int t[kNarrowRows], r[kNarrowRows];
+    narrow_pairs(p, n_pairs, k, M_cap, row_map, lane, t, r);
+    move_narrow<S>(x, s, t, r, lane, row16, n_s, out, s_out);
+  } else {
+    const int64_t t = p / k, r = row_map[p];
+    if (r >= 0 && r < M_cap) move_row<S>(x, s, t, r, lane, row16, n_s, out, s_out);
+  }
 }
 
 // Routing and rows in one launch: a workgroup takes kWaves * kPer (token, slot) pairs, finds the pairs of each
@@ -113,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void sort_rows_kernel(const u32x4* __rest
 // 29 / 38; 4096 x 256, 1024 experts, k = 1 10.4 / 12.7.  (8192 x 256, 8 experts, k = 1 14.8 / 12.6.)
 // Otherwise a launch in front has counted chunks of kChunk tokens, and a workgroup adds those up and counts in its own
 // chunk alone; it then takes two pairs a wave: 16384 x 2048, 64 experts, k = 16 one, two, four, eight 236 215 215 216,
-// 8192 x 256, 8 experts, k = 1 11.1 9.8 10.0 12.5, 4096 x 7168, 256 experts, k = 8 149 143 144 143 us.
+// 4096 x 7168, 256 experts, k = 8 149 143 144 143 us; of narrow rows kNarrowRows.
 constexpr int kMaxExperts = 1024, kMaxPairs = 4096;
 constexpr int kChunk = kRouteChunk, kPerCounted = 2;
 __global__ __launch_bounds__(kThreads) void chunk_count_kernel(const int32_t* __restrict__ topk_idx, int n_pairs, int k,
@@ -200,21 +247,39 @@ __global__ __launch_bounds__(kThreads) void route_sort_kernel(
   if (blockIdx.x == 0)
     for (int e = tid; e <= E; e += kThreads) offsets[e] = start[e];
   if (pad < 0) {
-    for (int i = 0; i < kPer; ++i) {
-      const int slot = __builtin_amdgcn_readfirstlane(wave) + i * kWaves, p = p0 + slot;
-      if (p >= n_pairs) return;
-      const int e = __builtin_amdgcn_readlane(mine, slot);
+    // pair `slot` of the workgroup, the same for all lanes: its row, -1 if there is none
+    auto row_of = [&](int slot) {
+      const int p = p0 + slot, e = __builtin_amdgcn_readlane(mine, slot);
       if (e < 0 || e >= E) {
         if (lane == 0) row_map[p] = -1;
-        continue;
+        return -1;
       }
-      const int64_t r = start[e] + before[e] + __popcll(__ballot(mine == e && lane < slot));
-      if (r >= M_cap) continue;
+      const int r = start[e] + before[e] + __popcll(__ballot(mine == e && lane < slot));
+      if (r >= M_cap) return -1;
       if (lane == 0) {
-        row_map[p] = (int)r;
+        row_map[p] = r;
         src_row[r] = p;
       }
-      move_row<S>(x, s, p / k, r, lane, row16, n_s, out, s_out);
+      return r;
+    };
+    const int w = __builtin_amdgcn_readfirstlane(wave);
+    if constexpr (kPer == kNarrowRows) {
+      if (p0 + w * kPer >= n_pairs) return;
+      int t[kPer], r[kPer];
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const int slot = w * kPer + j;
+        r[j] = p0 + slot < n_pairs ? row_of(slot) : -1;
+        t[j] = (p0 + slot < n_pairs ? p0 + slot : n_pairs - 1) / k;
+      }
+      move_narrow<S>(x, s, t, r, lane, row16, n_s, out, s_out);
+    } else {
+      for (int i = 0; i < kPer; ++i) {
+        const int slot = w + i * kWaves;
+        if (p0 + slot >= n_pairs) return;
+        const int r = row_of(slot);
+        if (r >= 0) move_row<S>(x, s, (p0 + slot) / k, r, lane, row16, n_s, out, s_out);
+      }
     }
   } else {
     const int e = pad / parts, part = pad - e * parts;
@@ -227,18 +292,69 @@ __global__ __launch_bounds__(kThreads) void route_sort_kernel(
 }
 
 // Sum of a dot product, fixed order: a lane's products in column order, then a butterfly over the wave.
-template <bool kDprobs>
+template <bool kDprobs, bool kIsNarrow>
 __global__ __launch_bounds__(kThreads) void return_bwd_kernel(
     const u32x4* __restrict__ dy, const float* __restrict__ row_w, int64_t row16, int n_pairs, int k, int parts,
     const int32_t* __restrict__ row_map, const int32_t* __restrict__ offsets, const int32_t* __restrict__ src_row,
     int64_t M_cap, u32x4* __restrict__ dy_perm, const u32x4* __restrict__ y_perm, float* __restrict__ dprobs) {
-  const int pad = (int)blockIdx.x - (n_pairs + kWaves - 1) / kWaves;
+  constexpr int kBlock = kWaves * (kIsNarrow ? kNarrowRows : 1);
+  const int pad = (int)blockIdx.x - (n_pairs + kBlock - 1) / kBlock;
   if (pad >= 0) {
     pad_rows<e8m0_t>(pad / parts, pad % parts, parts, offsets, src_row, M_cap, row16, 0, dy_perm, nullptr);
     return;
   }
-  const int p = pair_of_wave(), lane = threadIdx.x & 63;
+  const int p = pair_of_wave() * (kIsNarrow ? kNarrowRows : 1), lane = threadIdx.x & 63;
   if (p >= n_pairs) return;
+  // a piece of a token's gradient: weighted, and its part of the dot product
+  auto weigh = [](const u32x4& d, const u32x4& y, float w, float& acc) {
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float lo = bf16_lo(d[i]), hi = bf16_hi(d[i]);
+      o[i] = pack_bf16x2(w * lo, w * hi);
+      if (kDprobs) {
+        acc = fmaf(lo, bf16_lo(y[i]), acc);
+        acc = fmaf(hi, bf16_hi(y[i]), acc);
+      }
+    }
+    return o;
+  };
+  if constexpr (kIsNarrow) {
+    int t[kNarrowRows], r[kNarrowRows];
+    narrow_pairs(p, n_pairs, k, M_cap, row_map, lane, t, r);
+    const int q = p + lane % kNarrowRows < n_pairs ? p + lane % kNarrowRows : n_pairs - 1;
+    const float wq = row_w[q];
+    int any = r[0];
+#pragma unroll
+    for (int j = 1; j < kNarrowRows; ++j) any = r[j] > any ? r[j] : any;
+    if (any < 0) {  // every pair of the wave is dropped
+      if (kDprobs && lane < kNarrowRows && p + lane < n_pairs) dprobs[p + lane] = 0.0f;
+      return;
+    }
+    const int piece = lane < row16 ? lane : 0;
+    u32x4 y[kNarrowRows], d[kNarrowRows];
+#pragma unroll
+    for (int j = 0; j < kNarrowRows; ++j) {
+      if (kDprobs) y[j] = ldnt16(y_perm + (r[j] >= 0 ? r[j] : any) * row16 + piece);  // dropped: one that is read anyway
+      d[j] = ld16(dy + t[j] * row16 + piece);
+    }
+    float mine = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kNarrowRows; ++j) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wq), j));
+      float acc = 0.0f;
+      const u32x4 o = weigh(d[j], y[j], w, acc);
+      if (r[j] >= 0 && lane < row16) stnt16(dy_perm + r[j] * row16 + lane, o);
+      if (kDprobs) {
+        acc = r[j] >= 0 && lane < row16 ? acc : 0.0f;
+#pragma unroll
+        for (int b = 1; b < 64; b <<= 1) acc += __shfl_xor(acc, b);
+        mine = lane == j ? acc : mine;
+      }
+    }
+    if (kDprobs && lane < kNarrowRows && p + lane < n_pairs) dprobs[p + lane] = mine;
+    return;
+  }
   const int64_t t = p / k, r = row_map[p];
   float acc = 0.0f;
   if (r >= 0 && r < M_cap) {
@@ -254,16 +370,7 @@ __global__ __launch_bounds__(kThreads) void return_bwd_kernel(
 #pragma unroll
       for (int u = 0; u < kPieces; ++u)
         if (c0 + 64 * u < row16) {
-          u32x4 o;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float lo = bf16_lo(d[u][i]), hi = bf16_hi(d[u][i]);
-            o[i] = pack_bf16x2(w * lo, w * hi);
-            if (kDprobs) {
-              acc = fmaf(lo, bf16_lo(y[u][i]), acc);
-              acc = fmaf(hi, bf16_hi(y[u][i]), acc);
-            }
-          }
+          const u32x4 o = weigh(d[u], y[u], w, acc);
           stnt16(dy_perm + r * row16 + c0 + 64 * u, o);
         }
     }
@@ -276,12 +383,14 @@ __global__ __launch_bounds__(kThreads) void return_bwd_kernel(
 }
 
 // Whether routing and rows share a launch behind chunk counts (otherwise the routing has its own launches).  Every
-// workgroup of 16 pairs reads the counts and half a chunk, which pays while the workgroups are few and their rows long.
-// us, with / without: 100 tokens x 256 columns, 64 experts, k = 64 12 / 42; 1024 x 2048, 64, k = 8 12.5 / 18.5; 4096 x
-// 7168, 256, k = 8 143 / 153; 5001 x 7168 bytes, 32, k = 8 60 / 64.  Beyond: 32000 x 256, 8, k = 2 31 / 23; 8192 x 7168, 32, k
-// = 8 211 / 207, 16384 tokens 427 / 409; 16384 x 256, 64, k = 4 (4096 counts) 36 / 27.
+// workgroup of 16 pairs (64 of narrow rows) reads the counts and half a chunk, which pays while the workgroups are few
+// and their rows long.  us, with / without: 1024 tokens x 2048 columns, 64 experts, k = 8 12.5 / 18.5; 4096 x 7168, 256, k = 8
+// 143 / 153; 5001 x 7168 bytes, 32, k = 8 60 / 64; beyond 8192 x 7168, 32, k = 8 211 / 207, 16384 tokens 427 / 409.  Narrow: 700 x
+// 256, 512, k = 8 10.6 / 17.2; 4000 x 128, 8, k = 8 12.1 / 15.3; 8000 x 256, 64 17.9 / 20.2; 32000 x 256, 8, k = 2 16.1 / 17.1;
+// beyond 12000 x 128, 8, k = 8 22.6 / 19.6, 16000 27 / 21.
 bool counted(int64_t n_pairs, int64_t n_counts, int64_t row16) {
-  return n_pairs <= (row16 >= 256 ? 48 << 10 : 32 << 10) && n_pairs * n_counts <= (int64_t)1 << 27;
+  return n_pairs <= (row16 <= kNarrow ? 64 << 10 : row16 >= 256 ? 48 << 10 : 32 << 10) &&
+         n_pairs * n_counts <= (int64_t)1 << 27;
 }
 
 // Workgroups for an expert's padding (up to align - 1 rows of zeros): a wave a row, as long as there are no more than
@@ -292,7 +401,10 @@ int pad_parts(int E, int align, int64_t row16) {
   return row16 < 128 ? 1 : most < need ? most : need;
 }
 
-unsigned grid_of(int64_t n_pairs, int n_pad) { return (unsigned)(n_pad + (n_pairs + kWaves - 1) / kWaves); }
+unsigned grid_of(int64_t n_pairs, int n_pad, bool narrow) {
+  const int block = kWaves * (narrow ? kNarrowRows : 1);
+  return (unsigned)(n_pad + (n_pairs + block - 1) / block);
+}
 
 // With topk_idx the routing maps are built too.
 template <typename S>
@@ -302,6 +414,7 @@ hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_
   const u32x4* const in = static_cast<const u32x4*>(x);
   u32x4* const to = static_cast<u32x4*>(out);
   const int64_t n_pairs = T * k;
+  const bool narrow = row16 <= kNarrow;
   const int parts = pad_parts(E, topk_idx ? align : kTile, row16);  // (maps that are there may have any padding)
   if (topk_idx || T == 0) {
     const int64_t n_chunks = (T + kChunk - 1) / kChunk;
@@ -316,15 +429,19 @@ hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_
     }
     if (counted(n_pairs, n_chunks * E, row16)) {
       chunk_count_kernel<<<(unsigned)n_chunks, kThreads, 0, st>>>(topk_idx, (int)n_pairs, k, E, counts);
-      FF8_GO(kPerCounted, counts);
+      if (narrow)
+        FF8_GO(kNarrowRows, counts);
+      else
+        FF8_GO(kPerCounted, counts);
       return hipGetLastError();
     }
 #undef FF8_GO
     const hipError_t e = launch_route(topk_idx, T, k, E, align, row_map, offsets, src_row, M_cap, workspace, st);
     if (e != hipSuccess) return e;
   }
-  sort_rows_kernel<S><<<grid_of(n_pairs, E * parts), kThreads, 0, st>>>(in, s, row16, n_s, (int)n_pairs, k, parts,
-                                                                        row_map, offsets, src_row, M_cap, to, s_out);
+  auto* const f = narrow ? sort_rows_kernel<S, true> : sort_rows_kernel<S, false>;
+  f<<<grid_of(n_pairs, E * parts, narrow), kThreads, 0, st>>>(in, s, row16, n_s, (int)n_pairs, k, parts, row_map, offsets,
+                                                              src_row, M_cap, to, s_out);
   return hipGetLastError();
 }
 
@@ -353,15 +470,12 @@ hipError_t launch_unpermute_bwd(const uint16_t* dy, const float* row_w, int64_t 
                                 const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
                                 uint16_t* dy_perm, const uint16_t* y_perm, float* dprobs, hipStream_t st) {
   const int parts = pad_parts(E, kTile, H / 8);
-  const unsigned grid = grid_of(T * k, E * parts);
-  const u32x4 *d = reinterpret_cast<const u32x4*>(dy), *y = reinterpret_cast<const u32x4*>(y_perm);
-  u32x4* const o = reinterpret_cast<u32x4*>(dy_perm);
-  if (dprobs)
-    return_bwd_kernel<true><<<grid, kThreads, 0, st>>>(d, row_w, H / 8, (int)(T * k), k, parts, row_map, offsets, src_row,
-                                                       M_cap, o, y, dprobs);
-  else
-    return_bwd_kernel<false><<<grid, kThreads, 0, st>>>(d, row_w, H / 8, (int)(T * k), k, parts, row_map, offsets, src_row,
-                                                        M_cap, o, nullptr, nullptr);
+  const bool narrow = H / 8 <= kNarrow;
+  auto* const f = dprobs ? narrow ? return_bwd_kernel<true, true> : return_bwd_kernel<true, false>
+                         : narrow ? return_bwd_kernel<false, true> : return_bwd_kernel<false, false>;
+  f<<<grid_of(T * k, E * parts, narrow), kThreads, 0, st>>>(
+      reinterpret_cast<const u32x4*>(dy), row_w, H / 8, (int)(T * k), k, parts, row_map, offsets, src_row, M_cap,
+      reinterpret_cast<u32x4*>(dy_perm), reinterpret_cast<const u32x4*>(y_perm), dprobs);
   return hipGetLastError();
 }
 
