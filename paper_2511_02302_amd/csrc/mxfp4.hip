@@ -113,10 +113,13 @@ struct Weights {
       if (i % 2 == 0) s[i / 2] = ts + tile * kt * 64;
     }
   }
+  // kKeep: other workgroups will read the same, so that they are loaded as lines that stay in the L2.
+  template <bool kKeep>
   __device__ __forceinline__ void fetch(int64_t block, Block& b) const {
     const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) b.q[i] = ldnt16(q[i] + block * 1024 + lane * 16);
+    for (int i = 0; i < kTiles; ++i)
+      b.q[i] = kKeep ? ld16(q[i] + block * 1024 + lane * 16) : ldnt16(q[i] + block * 1024 + lane * 16);
 #pragma unroll
     for (int i = 0; i < kTiles / 2; ++i)
       b.s[i] = __builtin_nontemporal_load(reinterpret_cast<const uint16_t*>(s[i] + block * 128 + lane * 2));
@@ -160,7 +163,7 @@ __device__ __forceinline__ int x_place(int r, int p) { return r * 16 + (p ^ ((r 
 // One where the block has no row of data behind its fourth, four otherwise.  us, one / always four: 1 token, 32
 // experts, k = 8, 7168 x 2048 up 22.0 / 22.4, down 14.3 / 15.0; 4 tokens up 55.2 / 57.4; 7 tokens, 64 experts, k = 6,
 // 2048 x 1408 up 21.0 / 22.0, down 11.4 / 12.1.
-template <bool kSwiglu, int kWaves, int kX>
+template <bool kSwiglu, int kWaves, bool kKeep, int kX>
 __device__ __forceinline__ void few_rows(const uint16_t* __restrict__ x, int src, unsigned mask,
                                          const Weights<kSwiglu>& w, int wave, int64_t K, float* part) {
   const int lane = threadIdx.x & 63;
@@ -182,7 +185,7 @@ __device__ __forceinline__ void few_rows(const uint16_t* __restrict__ x, int src
   auto fetch = [&](int64_t i, int d) {
     const int64_t s = wave + i * kWaves;
     keep_order();
-    w.fetch(s, wb[d]);
+    w.template fetch<kKeep>(s, wb[d]);
 #pragma unroll
     for (int r = 0; r < kX; ++r) xb[d][r] = xp[r][s * 16];
     keep_order();
@@ -232,7 +235,7 @@ __device__ __forceinline__ void few_rows(const uint16_t* __restrict__ x, int src
   for (int i = 0; i < kTiles; ++i) *reinterpret_cast<f32x4*>(&part[i * 256 + lane * 4]) = acc[i];
 }
 
-template <bool kSwiglu, int kWaves>
+template <bool kSwiglu, int kWaves, bool kKeep>
 __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
     const uint16_t* __restrict__ x, int64_t x_rows, const uint8_t* __restrict__ tq, const uint8_t* __restrict__ ts,
     const int32_t* __restrict__ offsets, int E, const int32_t* __restrict__ src_row, int top_k, int64_t N, int64_t K,
@@ -255,9 +258,9 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
   const unsigned mask = (unsigned)__ballot(src >= 0) & 0xFFFFu;
   const Weights<kSwiglu> w(tq, ts, e, n0, N, K / kTile);
   if (mask & 0xFFF0u)
-    few_rows<kSwiglu, kWaves, 4>(x, src, mask, w, wave, K, part[wave]);
+    few_rows<kSwiglu, kWaves, kKeep, 4>(x, src, mask, w, wave, K, part[wave]);
   else if (mask)
-    few_rows<kSwiglu, kWaves, 1>(x, src, mask, w, wave, K, part[wave]);
+    few_rows<kSwiglu, kWaves, kKeep, 1>(x, src, mask, w, wave, K, part[wave]);
   __syncthreads();
   // elements q, q + 1: tile q / 256, token (q / 4) % 16, weight rows 4 ((q / 64) % 4) + q % 4 .. + 1 of the tile
   for (int q = 2 * threadIdx.x; q < kCols * 16; q += kWaves * 128) {
@@ -372,9 +375,9 @@ __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const 
 #pragma unroll
   for (int m = 0; m < kM; ++m) xb[m] = xp[m][0];
   keep_order();
-  w.fetch(0, wb[0]);
+  w.template fetch<false>(0, wb[0]);
   keep_order();
-  w.fetch(kt > 1 ? 1 : 0, wb[1]);
+  w.template fetch<false>(kt > 1 ? 1 : 0, wb[1]);
   keep_order();
 #pragma unroll
   for (int m = 0; m < kM; ++m) xs[x_place(16 * m + t16, piece)] = xb[m];
@@ -400,7 +403,7 @@ __device__ __forceinline__ void many_rows(const uint16_t* __restrict__ x, const 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (j == 3) {
-          w.fetch(w_next, wb[d]);
+          w.template fetch<false>(w_next, wb[d]);
           keep_order();
         }
         decode(j < 3 ? d : 1 - d, (j + 1) & 3, a[(j + 1) & 1]);
@@ -539,8 +542,14 @@ hipError_t launch_grouped_gemv_mxfp4(const uint16_t* x, int64_t x_rows, const ui
     // tokens 27.8 / 27.5; 7168, 16 tokens 80 / 76.  (With few blocks a wave has little to hide its start behind, and
     // more workgroups fit beside one another; with many, two waves have too few loads in flight.)
     const bool two = K <= 12 * kTile;
-    auto* const f = swiglu ? two ? gemv_mxfp4_kernel<true, 2> : gemv_mxfp4_kernel<true, 4>
-                           : two ? gemv_mxfp4_kernel<false, 2> : gemv_mxfp4_kernel<false, 4>;
+    // From 16 rows an expert on its weights are read by more than one row block.  us, kept in the L2 / not: 204 rows each
+    // on 4 experts, 6528 x 2 x 512 25.6 / 29.6, 38 on 7, 2304 x 2 x 640 9.4 / 9.8, 32 on 8, 4096 x 2 x 512 11.3 / 11.9; 8
+    // on 32, 7168 x 2 x 2048 87 / 82, one token 24.3 / 21.9.
+    const bool keep = rows >= 16 * (int64_t)E;
+    auto* const f = swiglu ? two ? keep ? gemv_mxfp4_kernel<true, 2, true> : gemv_mxfp4_kernel<true, 2, false>
+                                 : keep ? gemv_mxfp4_kernel<true, 4, true> : gemv_mxfp4_kernel<true, 4, false>
+                           : two ? keep ? gemv_mxfp4_kernel<false, 2, true> : gemv_mxfp4_kernel<false, 2, false>
+                                 : keep ? gemv_mxfp4_kernel<false, 4, true> : gemv_mxfp4_kernel<false, 4, false>;
     f<<<(unsigned)(M_cap / 16 * (N / (16 * kTiles))), two ? 128 : 256, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row,
                                                                                 top_k, N, K, out);
   }
