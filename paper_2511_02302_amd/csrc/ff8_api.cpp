@@ -106,7 +106,7 @@ static int permute_quant_dprobs_common(const char* fn, const ff8_bf16* dy, const
 
 extern "C" {
 
-int ff8_version(void) { return 100; }
+int ff8_version(void) { return 200; }
 
 const char* ff8_status_string(int status) {
   switch (status) {
