@@ -296,6 +296,8 @@ class ExpertLayerFP4:
         T = x.shape[0]
         if T > self.T:
             raise ValueError(f"a batch of {T} tokens, the layer was made for {self.T}")
+        if tuple(logits.shape) != (T, self.E):  # the router would take any number of experts
+            raise ValueError(f"logits must have shape {(T, self.E)}, got {tuple(logits.shape)}")
         b, M = self.buf, self.rows(T)
         idx, probs, row_map, y = b["topk_idx"][:T], b["probs"][:T], b["row_map"][:T], b["y"][:T]
         src, h, y_perm = b["src_row"][:M], b["h"][:M], b["y_perm"][:M]

@@ -165,3 +165,17 @@ def test_sizes_of_one_launch(lib):
     assert b"2^25" in lib.ff8_last_error()
     assert lib.ff8_quant_mxfp4(P, 1 << 27, 128, P, P, None) == SHAPE
     assert lib.ff8_grouped_gemv_mxfp4(P, 4, P, P, P, 4, P, 1, 1 << 21, 1 << 13, 128, P, None) == SHAPE
+
+
+@pytest.mark.parametrize("rows,experts", [(4, 16), (4, 9), (4, 7), (3, 8), (5, 8)])
+def test_serving_layer_checks_its_logits(rows, experts):
+    """The router takes the number of experts from the logits, the routing from the layer: of wider logits the
+    choices behind the layer's experts would be dropped without a word."""
+    torch = pytest.importorskip("torch")
+    from paper_2511_02302_amd.layer import ExpertLayerFP4
+    layer = ExpertLayerFP4(4, 256, 8, 2, 128, device="cpu")
+    x = torch.zeros((4, 256), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="logits must have shape"):
+        layer.forward(x, torch.zeros((rows, experts)))
+    with pytest.raises(ValueError, match="device tensor"):  # the right shape stops at the device check here
+        layer.forward(x, torch.zeros((4, 8)))
