@@ -19,6 +19,7 @@
 
 #include "ff8_device.hpp"
 #include "ff8_launch.hpp"
+#include "rows_rule.hpp"
 
 namespace ff8 {
 
@@ -26,10 +27,6 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kPadGroups = 512;
-// Rows of at most kNarrow pieces are moved kNarrowRows at a time by a wave.  us, so / one a wave, maps there and maps to be
-// built: 16000 tokens x 128 columns, 8 experts, k = 8 10.1 / 27.1 and 21 / 38, gradient 26.5 / 46; x 512, 32 experts 25.6 / 29.7,
-// 39 / 42, 53 / 58.  (Wider ones four or two at a time: 1024 columns 49 / 44, 2048 98 / 97.)
-constexpr int kNarrow = 64, kNarrowRows = 8;
 constexpr int kPieces = 8;  // 16-byte pieces that a lane has in flight
 
 // One wave: row r becomes token t's row, or a row of zeros (scales 2^-126).  row16: 16-byte pieces of a row; n_s:
@@ -155,13 +152,11 @@ __global__ __launch_bounds__(kThreads) void sort_rows_kernel(const u32x4* __rest
 // Routing and rows in one launch: a workgroup takes kWaves * kPer (token, slot) pairs, finds the pairs of each
 // expert and those before its own, and so knows the group offsets and its rows.  Behind those, others fill the
 // expert groups' padding.  Integer LDS atomics: the counts do not depend on order.
-// Up to kMaxPairs pairs every workgroup counts them all by itself.  us, so / with the routing in launches of its own:
-// 1024 tokens x 256 columns, 8 experts, k = 2 6.9 / 11.4; 512 x 7168, 64 experts, k = 8 17 / 26, with 128-row padding
-// 29 / 38; 4096 x 256, 1024 experts, k = 1 10.4 / 12.7.  (8192 x 256, 8 experts, k = 1 14.8 / 12.6.)
+// Up to kMaxPairs pairs every workgroup counts them all by itself (counts NULL).
 // Otherwise a launch in front has counted chunks of kChunk tokens, and a workgroup adds those up and counts in its own
 // chunk alone; it then takes two pairs a wave: 16384 x 2048, 64 experts, k = 16 one, two, four, eight 236 215 215 216,
 // 4096 x 7168, 256 experts, k = 8 149 143 144 143 us; of narrow rows kNarrowRows.
-constexpr int kMaxExperts = 1024, kMaxPairs = 4096;
+constexpr int kMaxExperts = 1024;
 constexpr int kChunk = kRouteChunk, kPerCounted = 2;
 __global__ __launch_bounds__(kThreads) void chunk_count_kernel(const int32_t* __restrict__ topk_idx, int n_pairs, int k,
                                                                int E, int32_t* __restrict__ counts) {
@@ -382,17 +377,6 @@ __global__ __launch_bounds__(kThreads) void return_bwd_kernel(
   }
 }
 
-// Whether routing and rows share a launch behind chunk counts (otherwise the routing has its own launches).  Every
-// workgroup of 16 pairs (64 of narrow rows) reads the counts and half a chunk, which pays while the workgroups are few
-// and their rows long.  us, with / without: 1024 tokens x 2048 columns, 64 experts, k = 8 12.5 / 18.5; 4096 x 7168, 256, k = 8
-// 143 / 153; 5001 x 7168 bytes, 32, k = 8 60 / 64; beyond 8192 x 7168, 32, k = 8 211 / 207, 16384 tokens 427 / 409.  Narrow: 700 x
-// 256, 512, k = 8 10.6 / 17.2; 4000 x 128, 8, k = 8 12.1 / 15.3; 8000 x 256, 64 17.9 / 20.2; 32000 x 256, 8, k = 2 16.1 / 17.1;
-// beyond 12000 x 128, 8, k = 8 22.6 / 19.6, 16000 27 / 21.
-bool counted(int64_t n_pairs, int64_t n_counts, int64_t row16) {
-  return n_pairs <= (row16 <= kNarrow ? 64 << 10 : row16 >= 256 ? 48 << 10 : 32 << 10) &&
-         n_pairs * n_counts <= (int64_t)1 << 27;
-}
-
 // Workgroups for an expert's padding (up to align - 1 rows of zeros): a wave a row, as long as there are no more than
 // kPadGroups, and one for rows below 2 KiB.  us, so / one each: 34 tokens x 6144, 24 experts, k = 7, padded to 128 9.5 /
 // 16.6; 199 x 4608, 27, k = 2 8.6 / 13.3; 300 x 1024, 8, k = 2 7.2 / 7.2.  With 256 at the most 9.8 and 8.7.
@@ -414,7 +398,7 @@ hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_
   const u32x4* const in = static_cast<const u32x4*>(x);
   u32x4* const to = static_cast<u32x4*>(out);
   const int64_t n_pairs = T * k;
-  const bool narrow = row16 <= kNarrow;
+  const bool narrow = narrow_rows(row16);
   const int parts = pad_parts(E, topk_idx ? align : kTile, row16);  // (maps that are there may have any padding)
   if (topk_idx || T == 0) {
     const int64_t n_chunks = (T + kChunk - 1) / kChunk;
@@ -423,11 +407,12 @@ hipError_t sort_rows(const void* x, const S* s, int64_t T, int64_t row16, int n_
   route_sort_kernel<S, PER><<<(unsigned)(E * parts + (n_pairs + kWaves * PER - 1) / (kWaves * PER)), kThreads, 0, st>>>(    \
       in, s, topk_idx, (int)n_pairs, k, E, align, parts, COUNTS, (int)n_chunks, row16, n_s, M_cap, row_map, offsets, \
       src_row, to, s_out)
-    if (n_pairs <= kMaxPairs) {
+    const SortForm form = sort_form(n_pairs, n_chunks * E, row16);
+    if (form == SortForm::kOneLaunch) {
       FF8_GO(1, nullptr);
       return hipGetLastError();
     }
-    if (counted(n_pairs, n_chunks * E, row16)) {
+    if (form == SortForm::kCounted) {
       chunk_count_kernel<<<(unsigned)n_chunks, kThreads, 0, st>>>(topk_idx, (int)n_pairs, k, E, counts);
       if (narrow)
         FF8_GO(kNarrowRows, counts);
@@ -470,7 +455,7 @@ hipError_t launch_unpermute_bwd(const uint16_t* dy, const float* row_w, int64_t 
                                 const int32_t* row_map, const int32_t* offsets, const int32_t* src_row, int64_t M_cap,
                                 uint16_t* dy_perm, const uint16_t* y_perm, float* dprobs, hipStream_t st) {
   const int parts = pad_parts(E, kTile, H / 8);
-  const bool narrow = H / 8 <= kNarrow;
+  const bool narrow = narrow_rows(H / 8);
   auto* const f = dprobs ? narrow ? return_bwd_kernel<true, true> : return_bwd_kernel<true, false>
                          : narrow ? return_bwd_kernel<false, true> : return_bwd_kernel<false, false>;
   f<<<grid_of(T * k, E * parts, narrow), kThreads, 0, st>>>(
