@@ -15,6 +15,7 @@
 
 #include "ff8_device.hpp"
 #include "ff8_launch.hpp"
+#include "mxfp4_rule.hpp"
 
 namespace ff8 {
 
@@ -91,7 +92,7 @@ __device__ __forceinline__ bf16x8_t decode8(uint32_t w, float scale) {
 // up rows beside them).  D = weights (16 x 32) times tokens^T (32 x 16): lane l holds token l % 16, weight rows
 // 4 (l / 16) .. + 3 of a tile.  The addresses are the same for all lanes but for the lane's own offset, so that they
 // stay in scalar registers.
-constexpr int kTiles = 4;
+constexpr int kTiles = kMxTiles;
 template <bool kSwiglu>
 struct Weights {
   const uint8_t *q[kTiles], *s[kTiles / 2];  // at the first column block of the rows
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
 // CU's are not another's.  Together they draw the clock from 2.45 to 1.97 GHz, so that the sum of cycles stays
 // near the larger of the two and the time does not.  Blocks of 48 or 64 rows and weights three blocks
 // ahead were slower.
-constexpr int kManyWaves = 4, kManyThreads = 64 * kManyWaves, kManyRows = 96;
+constexpr int kManyThreads = 64 * kManyWaves;
 
 // Workgroup b of a launch runs on XCD b % 8.  Each XCD takes an eighth of the (row block, weight rows) items, in
 // order: the workgroups that read the same rows of x, and those that read the same weights for two row blocks of
@@ -525,27 +526,13 @@ hipError_t launch_grouped_gemv_mxfp4(const uint16_t* x, int64_t x_rows, const ui
                                      int64_t N, int64_t K, bool swiglu, uint16_t* out, hipStream_t st) {
   const int64_t n_out = swiglu ? N / 2 : N;
   const int64_t cols = kManyWaves * kTiles * (swiglu ? 8 : 16), nt = (n_out + cols - 1) / cols;
-  // rows of all experts: T * top_k where the tokens are gathered, otherwise what 16-row padding leaves
-  const int64_t rows = top_k ? x_rows * top_k : M_cap - 15 * (int64_t)E;
-  // Blocks of 96 rows instead of 16 (times in us, 16 / 96):
-  //  * from 12 rows an expert on.  7168 wide, 32 experts, up projection: 8 rows 81 / 83, 12 92 / 84, 24 158 / 89;
-  //    2048 wide, 64 experts, down: 4 rows 24 / 23, 12 26 / 22; with skewed routing 8 rows 25 / 30, 12 33 / 28.
-  //  * and from 5/8 of an item per CU on: a workgroup of the 96-row form goes through all of K by itself.  4096 wide, 8
-  //    experts: 72 items 13 / 30, 144 7.6 / 11.5 and 44 / 46, 208 19 / 17, 232 80 / 54; 1024 wide: 116 18 / 19, 200 31 / 21.
-  if (rows >= 12 * (int64_t)E && (E + rows / kManyRows) * nt >= (int64_t)device_cu_count() * 5 / 8) {
+  const Mxfp4Form form = mxfp4_form(x_rows, top_k, M_cap, E, N, K, swiglu, device_cu_count());
+  if (form.many) {
     const int64_t blocks = M_cap / kManyRows + (E < M_cap / 16 ? E : M_cap / 16);
     auto* const f = swiglu ? gemm_mxfp4_kernel<true> : gemm_mxfp4_kernel<false>;
     f<<<(unsigned)((blocks * nt + 7) / 8 * 8), kManyThreads, 0, st>>>(x, x_rows, tq, ts, offsets, E, src_row, top_k, M_cap, N, K, out);
   } else {
-    // Two waves an item where K gives them at most six blocks each, otherwise four.  us, two waves / four: K = 1024,
-    // 32 experts, 8 and 32 tokens 8.4 / 9.8 and 9.8 / 11.3, 1408, 64 experts 13.2 / 14.1; 2048, one token 7.4 / 6.6, 32
-    // tokens 27.8 / 27.5; 7168, 16 tokens 80 / 76.  (With few blocks a wave has little to hide its start behind, and
-    // more workgroups fit beside one another; with many, two waves have too few loads in flight.)
-    const bool two = K <= 12 * kTile;
-    // From 16 rows an expert on its weights are read by more than one row block.  us, kept in the L2 / not: 204 rows each
-    // on 4 experts, 6528 x 2 x 512 25.6 / 29.6, 38 on 7, 2304 x 2 x 640 9.4 / 9.8, 32 on 8, 4096 x 2 x 512 11.3 / 11.9; 8
-    // on 32, 7168 x 2 x 2048 87 / 82, one token 24.3 / 21.9.
-    const bool keep = rows >= 16 * (int64_t)E;
+    const bool two = form.waves == 2, keep = form.keep;
     auto* const f = swiglu ? two ? keep ? gemv_mxfp4_kernel<true, 2, true> : gemv_mxfp4_kernel<true, 2, false>
                                  : keep ? gemv_mxfp4_kernel<true, 4, true> : gemv_mxfp4_kernel<true, 4, false>
                            : two ? keep ? gemv_mxfp4_kernel<false, 2, true> : gemv_mxfp4_kernel<false, 2, false>

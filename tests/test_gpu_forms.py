@@ -8,6 +8,7 @@ import torch
 from oracle import moe
 from paper_2511_02302_amd import ff8
 
+import test_gpu_mxfp4 as products
 import test_gpu_rows as rows
 from test_gpu_kernels import f64, host, poisoned
 
@@ -65,3 +66,61 @@ def test_return_dot_products(H):
     exact, size = (d * y).sum(2), (np.abs(d) * np.abs(y)).sum(2)
     assert np.all(np.abs(f64(dp) - exact) <= (8 * -(-H // 512) + 6) * 2.0 ** -24 * size)
     assert (f64(dp)[~kept] == 0).all()
+
+
+# SwiGLU, columns of out, K, align, real rows of the experts, form (as test_operator_forms.py numbers them)
+_FEW = [1, 0, 4, 5, 0, 16, 0, 2, 0, 0, 3, 0] * 3
+GROUPED = [(False, 640, 128, 16, products.MANY * 8, 1), (False, 1408, 384, 128, products.MANY * 4, 1),
+           (True, 384, 256, 16, products.MANY * 5, 1), (True, 640, 1664, 32, products.MANY * 3, 1),
+           (False, 384, 1536, 16, _FEW, 2), (True, 128, 1408, 16, _FEW, 2),
+           (False, 256, 1664, 16, _FEW, 4), (True, 384, 2048, 16, _FEW, 4),
+           (False, 128, 512, 16, [33, 17, 130], -2), (True, 256, 640, 128, [33, 0, 130], -2),
+           (False, 128, 4096, 64, [20, 40, 100], -4), (True, 128, 1792, 16, [20, 41, 97], -4)]
+
+
+@pytest.mark.parametrize("swiglu,n_out,K,align,counts,form", GROUPED)
+def test_grouped_rows_with_and_without_their_sources(swiglu, n_out, K, align, counts, form):
+    """Each form on grouped rows: padding skipped by src_row, or rows of zeros that are computed like any other."""
+    N, E = (2 * n_out if swiglu else n_out), len(counts)
+    w, tq, ts = products._weights(E, N, K, N + K)
+    offsets, src, M_cap = products._groups(counts, align, seed=1, extra=200)
+    pad = torch.from_numpy((src < 0) | (np.arange(M_cap) >= offsets[-1]))
+    x = products._bf16((M_cap, K), 4)
+    call = ff8.ff8_grouped_gemv_mxfp4_swiglu if swiglu else ff8.ff8_grouped_gemv_mxfp4
+    outs = []
+    for fill, sources in ((float("nan"), torch.from_numpy(src).cuda()), (0.0, None)):
+        x[pad] = fill  # padding rows are not read with src_row; behind the last group nothing is
+        x[int(offsets[-1]):] = float("nan")
+        outs.append(poisoned((M_cap, n_out), torch.bfloat16))
+        call(x.cuda(), tq, ts, torch.from_numpy(offsets).cuda(), outs[-1], src_row=sources)
+    torch.cuda.synchronize()
+    xs = np.nan_to_num(f64(x))
+    if swiglu:
+        products._swiglu_check(outs[0], xs, w, offsets, src, n_out)
+    else:
+        products._check_rows(outs[0], products.moe_product(xs, w, offsets), products._bound(xs, w, offsets), offsets, src)
+    assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
+
+
+# T, E, k, I, K, form: a decoding step's up projection
+GATHERED = [(1, 32, 8, 128, 2048, 4), (1, 8, 2, 256, 7168, 4), (5, 40, 3, 256, 1664, 4), (9, 12, 6, 128, 4096, 4),
+            (40, 32, 8, 128, 1792, 4), (4, 24, 5, 128, 1536, 2), (64, 4, 2, 128, 2048, -4), (33, 3, 3, 384, 896, -2),
+            (100, 16, 4, 1408, 384, 1)]
+
+
+@pytest.mark.parametrize("T,E,k,I,K,form", GATHERED)
+def test_swiglu_of_a_decoding_step(T, E, k, I, K, form):
+    idx = rows._idx(T, E, k, 0.0, seed=T)
+    _, offsets, _, s = moe.route(idx, E, 16)
+    M_cap = ff8.ff8_rows_bound_aligned(T, k, E, 16)
+    src = np.full(M_cap, 0x6BCDEF, dtype=np.int32)  # behind the last group anything may stand
+    src[:len(s)] = s
+    w, tq, ts = products._weights(E, 2 * I, K, I + K)
+    x = products._bf16((T, K), 6)
+    out = poisoned((M_cap, I), torch.bfloat16)
+    ff8.ff8_grouped_gemv_mxfp4_swiglu(x.cuda(), tq, ts, torch.from_numpy(np.asarray(offsets, np.int32)).cuda(), out,
+                                      src_row=torch.from_numpy(src).cuda(), top_k=k)
+    torch.cuda.synchronize()
+    m = int(offsets[-1])
+    xs = np.where(src[:m, None] >= 0, f64(x)[np.maximum(src[:m], 0) // k], 0.0)
+    products._swiglu_check(out, xs, w, offsets, src, I)
