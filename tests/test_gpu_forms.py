@@ -9,6 +9,7 @@ from oracle import moe
 from paper_2511_02302_amd import ff8
 
 import test_gpu_mxfp4 as products
+import test_gpu_router as gate
 import test_gpu_rows as rows
 from test_gpu_kernels import f64, host, poisoned
 
@@ -124,3 +125,21 @@ def test_swiglu_of_a_decoding_step(T, E, k, I, K, form):
     m = int(offsets[-1])
     xs = np.where(src[:m, None] >= 0, f64(x)[np.maximum(src[:m], 0) // k], 0.0)
     products._swiglu_check(out, xs, w, offsets, src, I)
+
+
+# Tokens, experts and k of the router's forms that its own tests leave out: 33 to 64 experts by k <= 16 and 65 to
+# 256 experts by k > 16, each with a bias and without; in bf16 also batches above 2048 tokens
+ROUTERS = [(70, 24, 5), (65, 31, 7), (40, 50, 16), (41, 64, 8), (31, 65, 17), (20, 100, 40), (9, 128, 33), (30, 127, 64),
+           (25, 129, 20), (12, 200, 64), (14, 255, 17), (17, 256, 32), (2060, 100, 6), (2050, 72, 4), (2049, 256, 3),
+           (3, 96, 2), (5, 192, 5)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("score,normalize", gate.MODES)
+def test_router(dtype, score, normalize, monkeypatch):
+    for with_bias in (False, True):
+        for n, (T, E, k) in enumerate(ROUTERS):
+            bias = torch.randn(E, generator=torch.Generator().manual_seed(n)) * 0.3 if with_bias else None
+            gate._check(gate._logits(T, E, dtype, 10 + n), bias, k, score, normalize)
+    monkeypatch.setattr(gate, "SHAPES", ROUTERS)
+    gate.test_backward(dtype, score, normalize)
