@@ -337,11 +337,13 @@ enum ff8_score {
 /*
  * ff8_router_topk -- the k experts of each token and their routing weights (the topk_idx and
  *   probs of ff8_permute_quant, ff8_unpermute and ff8_route) from the router's logits.
- *   logits   [T, E] float32.  -inf masks an expert; a NaN logit is never chosen (and makes the
- *            token's softmax weights NaN; with a bias and softmax scores that token chooses nothing).
+ *   logits   [T, E] float32.  -inf masks an expert; a NaN logit is never chosen, +inf is the largest.  Softmax scores
+ *            of a token with a NaN or +inf logit are NaN, and so are its weights (normalized ones, which are over the
+ *            chosen alone, only with a chosen +inf); with a bias such a token chooses nothing.
  *   bias     [E] float32 or NULL.  Experts are chosen by the largest score + bias (in float64; an expert whose
  *            bias is -inf or NaN is never chosen), or, without a bias, by the largest logit; equal ones by the lower index.
- *            The bias does not enter the weights.
+ *            The bias does not enter the weights.  The choice is among all E experts: a limit on groups of them
+ *            (node-limited routing) is not part of the call; -inf logits mask experts.
  *   topk_idx [T, k] int32, in descending order of choice; -1 where fewer than k experts can be chosen.
  *   probs    [T, k] float32: scale * score, or with normalize = 1 scale * score / (sum of the chosen
  *            scores); 0 where topk_idx is -1.  Normalized weights stay exact where the scores
@@ -416,7 +418,8 @@ int ff8_unpermute_bwd(const ff8_bf16* dy, const float* row_w, int64_t T, int64_t
  *   sign), two a byte with the lower column in the low nibble, and one UE8M0 scale for 32 columns.
  *   w [rows, cols] bf16, finite; q [rows, cols/2]; s [rows, cols/32].
  *   A group's T is the smallest integer >= -126 with max|w| <= 6 * 2^T (no value saturates; an all-zero group
- *   gets -126), the rule of the e4m3 scales; codes are rounded to nearest, ties to even, sign kept.
+ *   gets -126), the rule of the e4m3 scales; codes are rounded to nearest, ties to even, sign kept.  Magnitudes from
+ *   7 * 2^125 (2.98e38) on round up to 2^128, which no bf16 holds and the products below do not take.
  *   rows >= 1, cols a multiple of 128, rows * cols < 2^34.
  */
 int ff8_quant_mxfp4(const ff8_bf16* w, int64_t rows, int64_t cols, uint8_t* q, ff8_e8m0* s, void* stream);
@@ -445,6 +448,8 @@ int ff8_pack_mxfp4(const uint8_t* q, const ff8_e8m0* s, int64_t rows, int64_t co
  *   top_k    0: x [x_rows = M_cap, K] holds the grouped rows.  k >= 1: x [x_rows = T, K] holds the tokens, and row m
  *            takes token src_row[m] / top_k (src_row required): no permute is needed in front.
  *   out      [M_cap, N] bf16; rows >= offsets[E] untouched.
+ *   How the work is split goes by the buffers' sizes (top_k * x_rows, or M_cap), as the offsets are on the device; groups
+ *   of 16-row padding are the fastest, wider ones take up to 1.6 times as long with a few rows each.
  *   E <= 1024; M_cap, N, K multiples of 128; x_rows and M_cap below 2^31, x_rows * K below 2^35, M_cap * N below
  *   2^34; x, tq, ts and out 16-byte aligned.
  */

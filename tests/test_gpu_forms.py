@@ -143,3 +143,20 @@ def test_router(dtype, score, normalize, monkeypatch):
             gate._check(gate._logits(T, E, dtype, 10 + n), bias, k, score, normalize)
     monkeypatch.setattr(gate, "SHAPES", ROUTERS)
     gate.test_backward(dtype, score, normalize)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("score,normalize", gate.MODES)
+def test_router_of_infinite_logits(dtype, score, normalize):
+    """+inf is the largest logit.  Softmax scores of its token are NaN, as inf - inf is: with a bias it chooses nothing.
+    Sigmoid scores are 1.  A NaN logit leaves normalized weights of the others as they are."""
+    for E, k in ((12, 3), (60, 8), (200, 8), (100, 20), (600, 4)):
+        z = gate._logits(8, E, dtype, E)
+        z[0, E - 2] = float("inf")
+        z[1, [1, 5, E - 1]] = float("inf")
+        z[2] = float("inf")
+        z[3, 2], z[3, 3] = float("inf"), float("nan")
+        z[4, 7] = float("nan")
+        z[5, 0], z[5, 1] = float("inf"), -float("inf")
+        for bias in (None, torch.linspace(-0.3, 0.3, E)):
+            gate._check(z, bias, k, score, normalize)

@@ -37,3 +37,11 @@ def test_quant_error_and_pack():
     assert tq.shape == (4, 2, 64, 16) and ts.shape == (2, 2, 64, 2)
     assert np.array_equal(tq[1, 1, 35], q[16 + 3, 64 + 32: 64 + 48]) and ts[0, 1, 35, 1] == s[19, 4 + 2]
     assert np.array_equal(np.sort(tq.reshape(-1)), np.sort(q.reshape(-1)))
+
+
+def test_largest_magnitudes():
+    """From 7 * 2^125 on, values round up to 2^128, beyond bf16; the bf16 value below does not."""
+    w = np.zeros((1, 128))
+    w[0, 0], w[0, 32], w[0, 64] = 7 * 2.0 ** 125, -255 * 2.0 ** 120, 7 * 2.0 ** 125 - 2.0 ** 120
+    d = mxfp4.dequant(*mxfp4.quant(w))
+    assert d[0, 0] == 2.0 ** 128 and d[0, 32] == -2.0 ** 128 and d[0, 64] == 3 * 2.0 ** 126
