@@ -154,16 +154,17 @@ __device__ __forceinline__ int x_place(int r, int p) { return r * 16 + (p ^ ((r 
 // expert has to be looked up.  A wave brings its own piece of x through LDS into the order of the matrix
 // instruction; in registers it has two blocks of weights and x in flight.
 //
-// Bound by the weights' bytes.  One token of 7168 columns, 8 experts of 2 x 2048 rows with SwiGLU (125 MB): 21.0 us,
-// 5.9 TB/s, where a read of that size out of HBM takes 18.1; 7 tokens of 6 among 64 experts, 2048 x 1408 (49 MB): 11.4
-// us, 7.1 at the same rate, the rest being the launch and the first block of each wave.  Of the two blocks ahead:
-// three or more spill, and loads repeated behind a wave's last block, for a loop without its tail, cost 5 to 15%.
+// Bound by the weights' bytes.  One token of 7168 columns, 8 experts of 2 x 2048 rows with SwiGLU (125 MB): 21 to 22.5
+// us by box and session, 5.6 to 5.9 TB/s, where a read of that size out of HBM takes 18.1; 7 tokens of 6 among 64 experts,
+// 2048 x 1408 (49 MB): 11 to 12.6 us, 7.1 at the same rate, the rest being the launch and the first block of each wave.
+// Of the two blocks ahead: three or more spill, and loads repeated behind a wave's last block, for a loop without its
+// tail, cost 5 to 15%.
 //
 // The products of a wave's blocks, into its part of LDS.  kX: 16-byte pieces of x that a lane brings for a block,
 // four rows each; with one only the first four rows are there (the other columns of the products are not stored).
-// One where the block has no row of data behind its fourth, four otherwise.  us, one / always four: 1 token, 32
-// experts, k = 8, 7168 x 2048 up 22.0 / 22.4, down 14.3 / 15.0; 4 tokens up 55.2 / 57.4; 7 tokens, 64 experts, k = 6,
-// 2048 x 1408 up 21.0 / 22.0, down 11.4 / 12.1.
+// One where the block has no row of data behind its fourth, four otherwise.  us, one / always four, each pair in one
+// session: 1 token, 32 experts, k = 8, 7168 x 2048 up 22.4 / 23.0, down 14.6 / 15.1; 4 tokens 50.5 / 50.4 and 30.1 / 31.7;
+// 7 tokens, 64 experts, k = 6, 2048 x 1408 down 11.0 / 11.6.
 template <bool kSwiglu, int kWaves, bool kKeep, int kX>
 __device__ __forceinline__ void few_rows(const uint16_t* __restrict__ x, int src, unsigned mask,
                                          const Weights<kSwiglu>& w, int wave, int64_t K, float* part) {
@@ -295,12 +296,13 @@ __global__ __launch_bounds__(kWaves * 64, 3) void gemv_mxfp4_kernel(
 // wave goes through all column blocks and shares the block of x, which the workgroup brings into one of two LDS
 // buffers while it computes from the other.
 //
-// Bound by the matrix cores and the loads together: 32 experts with 32 rows on average, 7168 columns, 2 x 2048 rows
-// (511 MB): 131 to 138 us, 3.8 TB/s.  The loads alone take 94 us (74 at the rate of a large read), the matrix
-// instructions alone 101 (88 at that of a large product, 1370 TFLOP/s): experts' rows come in 16s, and one
-// CU's are not another's.  Together they draw the clock from 2.45 to 1.97 GHz, so that the sum of cycles stays
-// near the larger of the two and the time does not.  Blocks of 48 or 64 rows and weights three blocks
-// ahead were slower.
+// Bound by the matrix cores and the loads together: 256 tokens of 8 among 32 experts (64 rows on average), 7168 columns, 2
+// x 2048 rows (511 MB): 131 to 142 us by routing, 3.6 to 3.9 TB/s.  The loads alone take 94 us (74 at the rate of a large
+// read), the matrix instructions alone 101 (88 at that of a large product, 1370 TFLOP/s).  An expert's block of 45 to
+// 84 rows is computed in 16s: 2304 to 2320 rows for 2048.  With 64 rows on every expert the launch takes 117 us where that
+// session's random routing took 142: of the 25 us between them some 15 are the 13% more rows, the others that CUs get
+// unequal blocks.  The matrix cores are busy for 47% of the cycles and vector instructions (decoding) for 32%, at
+// 2.1 GHz (2.4 where less is busy).  Blocks of 48 or 64 rows and weights three blocks ahead were slower.
 constexpr int kManyThreads = 64 * kManyWaves;
 
 // Workgroup b of a launch runs on XCD b % 8.  Each XCD takes an eighth of the (row block, weight rows) items, in
