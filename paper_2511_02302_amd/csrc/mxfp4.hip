@@ -155,7 +155,7 @@ __device__ __forceinline__ int x_place(int r, int p) { return r * 16 + (p ^ ((r 
 // instruction; in registers it has two blocks of weights and x in flight.
 //
 // Bound by the weights' bytes.  One token of 7168 columns, 8 experts of 2 x 2048 rows with SwiGLU (125 MB): 21 to 22.5
-// us by box and session, 5.6 to 5.9 TB/s, where a read of that size out of HBM takes 18.1; 7 tokens of 6 among 64 experts,
+// us from card to card, 5.6 to 5.9 TB/s, where a read of that size out of HBM takes 18.1; 7 tokens of 6 among 64 experts,
 // 2048 x 1408 (49 MB): 11 to 12.6 us, 7.1 at the same rate, the rest being the launch and the first block of each wave.
 // Of the two blocks ahead: three or more spill, and loads repeated behind a wave's last block, for a loop without its
 // tail, cost 5 to 15%.
